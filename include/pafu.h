@@ -52,7 +52,9 @@ enum {
     PAFU_ERR_MISALIGNED = 5,         /* a device pointer is not 16-byte aligned */
     PAFU_ERR_CUDA = 6,               /* a CUDA runtime/driver call failed (launch error, no device) */
     PAFU_ERR_TIMEOUT = 7,            /* a bounded device-side wait ran out (pafu_workspace_status) */
-    PAFU_ERR_TOO_LARGE = 8           /* exceeds pafu_chunk_attn_noalloc's built-in scratch, or a pafu_cache's capacity */
+    PAFU_ERR_TOO_LARGE = 8,          /* exceeds pafu_chunk_attn_noalloc's built-in scratch, or a pafu_cache's capacity */
+    PAFU_ERR_BAD_PAGE = 9,           /* on the device: a page, slot or length that the paged cache does not have (pafu_workspace_status) */
+    PAFU_ERR_NO_PAGES = 10           /* on the device: too few free pages, or places in the slot map (pafu_workspace_status) */
 };
 
 /* Activation between the two linear layers of the salience head. */
@@ -116,9 +118,11 @@ pafu_status pafu_kept_counts(const pafu_shape* shape, const pafu_policy* policy,
 size_t pafu_workspace_bytes(const pafu_shape* shape, const pafu_policy* policy,
                             const pafu_head* head);
 
-/* Reads the workspace's status header.  SYNCHRONISES `stream` (one 4-byte device-to-host
+/* Reads the workspace's status header.  SYNCHRONISES `stream` (one small device-to-host
  * copy).  Returns PAFU_OK, or PAFU_ERR_TIMEOUT if a kernel gave up on a bounded wait since
- * the header was last zeroed (the outputs of that launch are then undefined). */
+ * the header was last zeroed (the outputs of that launch are then undefined), or
+ * PAFU_ERR_BAD_PAGE / PAFU_ERR_NO_PAGES if a kernel of the paged cache met one since then
+ * (see each call for what it did). */
 pafu_status pafu_workspace_status(const void* ws, void* stream);
 
 /* Diagnostic counters of the workspace's status header, accumulated by pafu_chunk_attn (d_head
@@ -374,6 +378,106 @@ pafu_status pafu_cache_update(pafu_cache* cache, const pafu_head* head,
                               const uint16_t* Qs, const uint16_t* Ks, const uint16_t* Vs,
                               const uint16_t* const* Knew, const uint16_t* const* Vnew, int64_t chunk,
                               int32_t* pruned, void* ws, size_t ws_bytes, void* stream);
+
+/* ---- Paged cache: many requests in one pool, one new token at a time --------------------------
+ * The calls above hold a stream's cache in one buffer and take its geometry from the host.  Where many requests of different
+ * lengths come and go, the cache is a pool of pages instead: a page holds page_size tokens of one request, a block
+ * table lists each request's pages in order, and token t of request r lies in page table[r][t / page_size], place
+ * t % page_size.  Lengths, tables, free pages and slots stay on the device: a step is
+ *     pafu_paged_tables -> (the layers' projections) -> per layer: pafu_paged_append, pafu_paged_attn
+ * with nothing read back, and a captured CUDA graph of it follows the lengths. */
+
+/* Element types.  Queries, new rows and outputs are bf16 or fp16; the pools hold the same type, or 8-bit floating point
+ * (e4m3: 4 exponent bits, 3 mantissa bits, largest value 448) with one scale a key head: value = stored * scale. */
+enum { PAFU_TYPE_BF16 = 0, PAFU_TYPE_F16 = 1, PAFU_TYPE_E4M3 = 2 };
+
+/* One layer's pools and the tables of all requests.  Element (page p, place i, head h, component d) of K lies at
+ * K[p * page_stride + i * token_stride + h * head_stride + d], of V likewise, so pages may be laid out token by token
+ * ([n_pages, page_size, n_kv_heads, d_head]), head by head, or as parts of larger tensors; rows of different (p, i, h) must not overlap.
+ * Supported: d_head 64 or 128; n_heads % n_kv_heads == 0, n_heads <= 65536; page_size * max_pages <= 2^30 and
+ * page_size * n_pages < 2^31; strides non-negative multiples of 16 bytes; each pool within 64 GiB. */
+typedef struct pafu_paged_cache {
+    int32_t n_heads;               /* query heads; heads [h * G, (h + 1) * G) share key head h, G = n_heads / n_kv_heads */
+    int32_t n_kv_heads;
+    int32_t d_head;
+    int32_t type;                  /* of queries, new rows and outputs: PAFU_TYPE_BF16 or PAFU_TYPE_F16 */
+    int32_t cache_type;            /* of the pools: the same, or PAFU_TYPE_E4M3 */
+    int32_t page_size;             /* tokens a page, any number >= 1 */
+    int32_t max_pages;             /* columns of the block table */
+    int32_t n_requests;            /* rows of the block table */
+    int64_t n_pages;               /* pages of the pools */
+    int64_t page_stride, token_stride, head_stride;    /* in elements of the pools */
+    void* K;                       /* device, 16-byte aligned */
+    void* V;
+    const float* k_scale;          /* device fp32 [n_kv_heads], positive; NULL = 1.  Only with PAFU_TYPE_E4M3 */
+    const float* v_scale;
+    int32_t* table;                /* device int32 [n_requests, max_pages], contiguous; NULL if n_requests is 0 */
+} pafu_paged_cache;
+
+/* Workspace of the three calls below: PAFU_PAGED_HEADER_BYTES that the caller zeroes once after allocating (the status
+ * header that pafu_workspace_status reads, and counters that are zero again at the end of every call), then scratch.
+ * 256-byte aligned.  It serves caches of the same d_head and any other geometry (0 = invalid cache), one call at a time: calls that may
+ * overlap on the GPU - two streams, two captured graphs that run side by side - need a workspace each.  It is not for the
+ * calls above: what those leave behind the header would be taken for counters. */
+#define PAFU_PAGED_HEADER_BYTES 4608
+size_t pafu_paged_workspace_bytes(const pafu_paged_cache* cache);
+
+/* Block tables and slot map of a step, from the requests' lengths.  With P(x) = ceil(x / page_size):
+ *   - a request that shrinks (ends: new length 0; takes back tokens: any smaller one) gives pages
+ *     table[r][P(new) .. P(old)) back; these table entries stay as they are and mean nothing any more;
+ *   - a request that grows gets P(new) - P(old) pages, written to table[r][P(old) .. P(new));
+ *   - free_list is a stack of *n_free page numbers, its top at the end.  What is given back is pushed first (requests in
+ *     order, each one's pages in order), then the pages needed are popped (requests in order, pages in order);
+ *   - the new tokens of all requests, in order, get the slots
+ *     table[r][t / page_size] * page_size + t % page_size for t in [old, new).
+ *   len_old, len_new  device int32 [n_requests], tokens before and after
+ *   free_list         device int32 [n_pages], in/out; entries above the new top are left as they were
+ *   n_free            device int32, in
+ *   n_free_out        device int32, out; may be n_free itself
+ *   len_out           device int32 [n_requests], out: len_new; may be len_old or len_new itself
+ *   slots             device int64 [n_slots], out; -1 behind the step's last new token
+ *   cu_new            device int32 [n_requests + 1], out: prefix sums of the new tokens
+ * All or nothing: with too few pages (those given back included) or more new tokens than n_slots, or with a length that
+ * is negative or needs more than max_pages pages, or a *n_free outside [0, n_pages], no page changes hands: table,
+ * free_list and the number of free pages stay, len_out = len_old, slots are all -1, cu_new all 0, and pafu_workspace_status reports
+ * PAFU_ERR_NO_PAGES (the first two) or PAFU_ERR_BAD_PAGE (the others).
+ * Apart from the aliases named, outputs must not overlap anything else.  Of `cache` only page_size, max_pages, n_requests, n_pages
+ * and table are looked at beyond the checks. */
+pafu_status pafu_paged_tables(const pafu_paged_cache* cache, const int32_t* len_old, const int32_t* len_new,
+                              int32_t* free_list, const int32_t* n_free, int32_t* n_free_out, int32_t* len_out,
+                              int64_t* slots, int64_t n_slots, int32_t* cu_new, void* ws, size_t ws_bytes, void* stream);
+
+/* New tokens' key and value rows into the pools: row i goes to slot slots[i] (page slots[i] / page_size, place
+ * slots[i] % page_size), rows with a negative slot go nowhere.  16-bit pools of the rows' type take copies, bit for bit; e4m3 pools take
+ * x * (1 / scale) rounded to the nearest e4m3 value, ties to even, beyond 448 (infinities too) to 448, NaN to NaN.
+ * A slot past the pool is left out and reported (PAFU_ERR_BAD_PAGE).  Where two rows name the same slot, what it holds
+ * afterwards is not defined.
+ *   Kn, Vn    device [n_tokens, n_kv_heads, d_head] of cache->type with strides ld_token and ld_head in elements (multiples of 8),
+ *             16-byte aligned, e.g. parts of fused query/key/value rows; they must not overlap the pools
+ *   slots     device int64 [n_tokens]
+ * n_tokens * n_kv_heads < 2^31. */
+pafu_status pafu_paged_append(const pafu_paged_cache* cache, const void* Kn, const void* Vn, int64_t ld_token, int64_t ld_head,
+                              const int64_t* slots, int64_t n_tokens, void* ws, size_t ws_bytes, void* stream);
+
+/* Attention of one new token a request over its pages (the operator of pafu_chunk_attn for a single query row and grouped
+ * heads): o[r,n] = sum_j softmax_j(scale * q[r,n] . k_j) v_j over the kept positions j of request r's lens[r] tokens.  The new token's
+ * own key and value are among them once pafu_paged_append has written them and lens counts them.
+ * n_recent < 0 keeps every position; otherwise the n_sink first and the n_recent last ones (the attention-sink prefix and the recent
+ * window of pafu_policy) are kept.  Positions outside are not read, whatever they hold.
+ * fp32 accumulation and softmax; the probabilities enter the product as 16-bit values, with what that rounding leaves over
+ * as a second term for bf16 pools and wherever G % 16 is in 1..8 or G <= 8.
+ *   Q         device [n_requests, n_heads, d_head] of cache->type with strides q_token and q_head in elements (multiples of 8), 16-byte
+ *             aligned
+ *   lens      device int32 [n_requests]
+ *   scale     softmax scale; 0 means 1 / sqrt(d_head)
+ *   O         device [n_requests, n_heads, d_head] of cache->type, contiguous, out
+ *   LSE       device fp32 [n_heads, n_requests] log-sum-exp of the scaled logits, or NULL
+ * A request without kept positions gets o = 0 and LSE = -inf.  Table entries that are no page of the pool are left out with their
+ * tokens, lengths outside [0, max_pages * page_size] are cut to it, and both are reported (PAFU_ERR_BAD_PAGE).  The work is cut evenly
+ * over the GPU whatever the lengths; results do not depend on timing.  n_requests * n_heads < 2^31. */
+pafu_status pafu_paged_attn(const pafu_paged_cache* cache, const void* Q, int64_t q_token, int64_t q_head, const int32_t* lens,
+                            int64_t n_sink, int64_t n_recent, float scale, void* O, float* LSE,
+                            void* ws, size_t ws_bytes, void* stream);
 
 /* Teacher-side salience target - Spatialtemporal-balanced Salience Estimation (Sec. 3.2, Eq. 4
  * and Eq. 5; Algorithm 3).  With P = softmax(scale * Q K^T) per head over the whole sequence of L

@@ -9,4 +9,5 @@ from .binding import (  # noqa: F401
     pafu_select, pafu_compact, pafu_compact_layers, pafu_cache_update, Cache, pafu_chunk_attn, pafu_chunk_attn_indexed, pafu_chunk_attn_noalloc, pafu_step, pafu_step_indexed,
     pafu_step_host, pafu_step_host_async,
     pafu_step_host_arena_bytes, pafu_sse, pafu_sse_mean_first, pafu_sse_workspace_bytes, pafu_step_timed, event_handles, step_args, lib,
+    PagedCache, pafu_paged_workspace_bytes, pafu_paged_tables, pafu_paged_append, pafu_paged_attn,
 )

@@ -24,12 +24,13 @@ FINAL_NONE, FINAL_SIGMOID = 0, 1
 STATUS_NAMES = {0: "PAFU_OK", 1: "PAFU_ERR_INVALID_ARG", 2: "PAFU_ERR_BAD_BUDGET",
                 3: "PAFU_ERR_UNSUPPORTED_SHAPE", 4: "PAFU_ERR_WORKSPACE_TOO_SMALL",
                 5: "PAFU_ERR_MISALIGNED", 6: "PAFU_ERR_CUDA", 7: "PAFU_ERR_TIMEOUT",
-                8: "PAFU_ERR_TOO_LARGE"}
+                8: "PAFU_ERR_TOO_LARGE", 9: "PAFU_ERR_BAD_PAGE", 10: "PAFU_ERR_NO_PAGES"}
 
 EXPORTS = ["pafu_version", "pafu_status_string", "pafu_kept_counts", "pafu_workspace_bytes",
            "pafu_workspace_status", "pafu_workspace_counters", "pafu_score", "pafu_score_qkv", "pafu_select", "pafu_compact",
            "pafu_chunk_attn", "pafu_chunk_attn_indexed", "pafu_chunk_attn_noalloc", "pafu_step", "pafu_step_indexed", "pafu_step_timed", "pafu_step_host_arena_bytes", "pafu_step_host", "pafu_step_host_async",
-           "pafu_sse_workspace_bytes", "pafu_sse", "pafu_sse_mean_first", "pafu_compact_layers", "pafu_cache_update"]
+           "pafu_sse_workspace_bytes", "pafu_sse", "pafu_sse_mean_first", "pafu_compact_layers", "pafu_cache_update",
+           "pafu_paged_workspace_bytes", "pafu_paged_tables", "pafu_paged_append", "pafu_paged_attn"]
 
 
 class PafuError(RuntimeError):
@@ -66,6 +67,15 @@ class CCache(ctypes.Structure):
                 ("cur", ctypes.c_int32), ("capacity", ctypes.c_int64), ("n_sink", ctypes.c_int64),
                 ("T", ctypes.c_int64), ("K", ctypes.c_void_p * 2), ("V", ctypes.c_void_p * 2),
                 ("SL", ctypes.c_void_p * 2), ("idx", ctypes.c_void_p)]
+
+
+class CPagedCache(ctypes.Structure):
+    _fields_ = [("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("d_head", ctypes.c_int32),
+                ("type", ctypes.c_int32), ("cache_type", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("n_requests", ctypes.c_int32), ("n_pages", ctypes.c_int64),
+                ("page_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("table", ctypes.c_void_p)]
 
 
 class CStepArgs(ctypes.Structure):
@@ -147,6 +157,15 @@ def lib() -> ctypes.CDLL:
         L.pafu_step_host.argtypes = [ctypes.POINTER(CStepArgs), vp, sz, vp]
         L.pafu_step_host_async.restype = i32
         L.pafu_step_host_async.argtypes = [ctypes.POINTER(CStepArgs), vp, sz, vp, vp]
+        pc = ctypes.POINTER(CPagedCache)
+        L.pafu_paged_workspace_bytes.restype = sz
+        L.pafu_paged_workspace_bytes.argtypes = [pc]
+        L.pafu_paged_tables.restype = i32
+        L.pafu_paged_tables.argtypes = [pc, vp, vp, vp, vp, vp, vp, vp, i64, vp, vp, sz, vp]
+        L.pafu_paged_append.restype = i32
+        L.pafu_paged_append.argtypes = [pc, vp, vp, i64, i64, vp, i64, vp, sz, vp]
+        L.pafu_paged_attn.restype = i32
+        L.pafu_paged_attn.argtypes = [pc, vp, i64, i64, vp, i64, i64, ctypes.c_float, vp, vp, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -342,6 +361,96 @@ def pafu_chunk_attn_noalloc(Q, Kc, Vc, cu_B, Kq, Vq, shape: Shape, scale: float,
     _check(lib().pafu_chunk_attn_noalloc(_ptr(Q), _ptr(Kc), _ptr(Vc), _ptr(cu_B), _ptr(Kq), _ptr(Vq),
                                          ctypes.byref(shape.c), float(scale), _ptr(O), _ptr(LSE),
                                          _stream()), "pafu_chunk_attn_noalloc")
+
+
+_PAGED_TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float8_e4m3fn: 2}
+
+
+def _need(ok: bool, where: str) -> None:
+    """An argument that the C entry point cannot see is wrong (a tensor's type, size or device)."""
+    if not ok:
+        raise PafuError(1, where)
+
+
+class PagedCache:
+    """One layer's paged key/value cache: pools K and V [n_pages, page_size, n_kv_heads, d_head] (any strides with contiguous
+    rows, the same for both; bf16, fp16 or float8_e4m3fn), the block table [n_requests, max_pages] int32, and for 8-bit pools
+    a scale a key head.  n_heads query heads share the key heads in groups; dtype is the type of
+    queries, new rows and outputs (default: the pools').  Only pointers are kept beside the tensors, so they are
+    updated in place."""
+
+    def __init__(self, K: torch.Tensor, V: torch.Tensor, table: torch.Tensor, n_heads: int,
+                 dtype: Optional[torch.dtype] = None, k_scale: Optional[torch.Tensor] = None,
+                 v_scale: Optional[torch.Tensor] = None):
+        where = "PagedCache"
+        if dtype is None:
+            dtype = torch.bfloat16 if K.dtype == torch.float8_e4m3fn else K.dtype
+        _need(K.dim() == 4 and K.shape == V.shape and K.stride() == V.stride() and K.dtype == V.dtype
+              and K.dtype in _PAGED_TYPES and (K.dtype == dtype or K.dtype == torch.float8_e4m3fn)
+              and dtype in (torch.bfloat16, torch.float16) and (K.stride(3) == 1 or K.shape[3] == 1), where)
+        _need(table.dim() == 2 and table.dtype == torch.int32 and table.is_contiguous(), where)
+        n_pages, page_size, n_kv, d = K.shape
+        for s in (k_scale, v_scale):
+            _need(s is None or (s.dtype == torch.float32 and s.shape == (n_kv,) and s.is_contiguous() and s.device == K.device), where)
+        _need(K.device == V.device == table.device, where)
+        self.K, self.V, self.table, self.k_scale, self.v_scale = K, V, table, k_scale, v_scale
+        self.dtype, self.device, self.n_heads, self.n_kv_heads, self.d_head = dtype, K.device, n_heads, n_kv, d
+        self.page_size, self.n_pages, self.n_requests, self.max_pages = page_size, n_pages, table.shape[0], table.shape[1]
+        self.c = CPagedCache(n_heads, n_kv, d, _PAGED_TYPES[dtype], _PAGED_TYPES[K.dtype], page_size, table.shape[1],
+                             table.shape[0], n_pages, K.stride(0), K.stride(1), K.stride(2), K.data_ptr(), V.data_ptr(),
+                             None if k_scale is None else k_scale.data_ptr(),
+                             None if v_scale is None else v_scale.data_ptr(), table.data_ptr())
+        self._ref = ctypes.byref(self.c)
+
+
+def _paged_stream(cache: PagedCache, where: str, *tensors) -> int:
+    """The current stream; every tensor must lie on the cache's device, and that must be the current one."""
+    dev = cache.device
+    for t in tensors:
+        _need(t is None or t.device == dev, where)
+    _need(dev.type == "cuda" and dev.index == torch.cuda.current_device(), where)
+    return _stream()
+
+
+def pafu_paged_workspace_bytes(cache: PagedCache) -> int:
+    return lib().pafu_paged_workspace_bytes(cache._ref)
+
+
+def pafu_paged_tables(cache: PagedCache, len_old: torch.Tensor, len_new: torch.Tensor, free_list: torch.Tensor,
+                      n_free: torch.Tensor, n_free_out: torch.Tensor, len_out: torch.Tensor, slots: torch.Tensor,
+                      cu_new: torch.Tensor, ws: torch.Tensor) -> None:
+    """Block tables and slot map of a step from the lengths before and after it, all on the device."""
+    where, R, i32 = "pafu_paged_tables", cache.n_requests, torch.int32
+    _need(len_old.dtype == i32 and len_new.dtype == i32 and len_out.dtype == i32 and free_list.dtype == i32
+          and n_free.dtype == i32 and n_free_out.dtype == i32 and cu_new.dtype == i32 and slots.dtype == torch.int64, where)
+    _need(len_old.numel() == R and len_new.numel() == R and len_out.numel() == R and cu_new.numel() == R + 1
+          and free_list.numel() == cache.n_pages and n_free.numel() == 1 and n_free_out.numel() == 1, where)
+    st = _paged_stream(cache, where, len_old, len_new, free_list, n_free, n_free_out, len_out, slots, cu_new, ws)
+    _check(lib().pafu_paged_tables(cache._ref, _ptr(len_old), _ptr(len_new), _ptr(free_list), _ptr(n_free), _ptr(n_free_out),
+                                   _ptr(len_out), _ptr(slots), slots.numel(), _ptr(cu_new), _ptr(ws),
+                                   ws.numel() * ws.element_size(), st), where)
+
+
+def pafu_paged_append(cache: PagedCache, Kn: torch.Tensor, Vn: torch.Tensor, slots: torch.Tensor, ws: torch.Tensor) -> None:
+    """New tokens' rows Kn, Vn [n, n_kv_heads, d_head] (equal strides, contiguous rows) into the slots they are given."""
+    where, n = "pafu_paged_append", slots.numel()
+    _need(Kn.shape == (n, cache.n_kv_heads, cache.d_head) and Vn.shape == Kn.shape and Vn.stride() == Kn.stride()
+          and Kn.dtype == cache.dtype and Vn.dtype == cache.dtype and Kn.stride(2) == 1 and slots.dtype == torch.int64, where)
+    st = _paged_stream(cache, where, Kn, Vn, slots, ws)
+    _check(lib().pafu_paged_append(cache._ref, Kn.data_ptr(), Vn.data_ptr(), Kn.stride(0), Kn.stride(1), _ptr(slots), n, _ptr(ws),
+                                   ws.numel() * ws.element_size(), st), where)
+
+
+def pafu_paged_attn(cache: PagedCache, Q: torch.Tensor, lens: torch.Tensor, O: torch.Tensor, LSE: Optional[torch.Tensor] = None,
+                    n_sink: int = 0, n_recent: int = -1, scale: float = 0.0, ws: Optional[torch.Tensor] = None) -> None:
+    """Attention of one new token a request, Q [n_requests, n_heads, d_head], over its pages."""
+    where, shape = "pafu_paged_attn", (cache.n_requests, cache.n_heads, cache.d_head)
+    _need(Q.shape == shape and O.shape == shape and Q.dtype == cache.dtype and O.dtype == cache.dtype and Q.stride(2) == 1
+          and lens.dtype == torch.int32 and lens.numel() == shape[0], where)
+    _need(LSE is None or (LSE.dtype == torch.float32 and LSE.numel() == shape[0] * shape[1]), where)
+    st = _paged_stream(cache, where, Q, lens, O, LSE, ws)
+    _check(lib().pafu_paged_attn(cache._ref, Q.data_ptr(), Q.stride(0), Q.stride(1), _ptr(lens), n_sink, n_recent, scale, _ptr(O),
+                                 _ptr(LSE), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(), st), where)
 
 
 def step_args(shape: Shape, head: Head, policy, K, V, Q, Kq, Vq, scale, scores, idx, Kc, Vc, SLc,

@@ -4,6 +4,7 @@
 #include <string.h>
 
 #include "common.cuh"
+#include "paged.cuh"
 
 namespace pafu {
 
@@ -97,6 +98,8 @@ const char* pafu_status_string(pafu_status s) {
         case PAFU_ERR_CUDA: return "CUDA call failed";
         case PAFU_ERR_TIMEOUT: return "bounded device wait ran out";
         case PAFU_ERR_TOO_LARGE: return "problem exceeds the built-in scratch of the no-allocation entry point";
+        case PAFU_ERR_BAD_PAGE: return "a page, slot or length that the paged cache does not have";
+        case PAFU_ERR_NO_PAGES: return "too few free pages or places in the slot map";
         default: return "unknown status";
     }
 }
@@ -132,11 +135,13 @@ size_t pafu_workspace_bytes(const pafu_shape* shape, const pafu_policy* policy, 
 
 pafu_status pafu_workspace_status(const void* ws, void* stream) {
     if (ws == nullptr) return PAFU_ERR_INVALID_ARG;
-    int32_t word = 0;
+    int32_t words[2] = {0, 0};
+    static_assert(kStatusWordTimeout == 0 && kStatusWordPaged == 1, "both words are read with one copy");
     cudaStream_t cs = static_cast<cudaStream_t>(stream);
-    if (cudaMemcpyAsync(&word, ws, sizeof word, cudaMemcpyDeviceToHost, cs) != cudaSuccess) return PAFU_ERR_CUDA;
+    if (cudaMemcpyAsync(words, ws, sizeof words, cudaMemcpyDeviceToHost, cs) != cudaSuccess) return PAFU_ERR_CUDA;
     if (cudaStreamSynchronize(cs) != cudaSuccess) return PAFU_ERR_CUDA;
-    return word == 0 ? PAFU_OK : PAFU_ERR_TIMEOUT;
+    if (words[0] != 0) return PAFU_ERR_TIMEOUT;
+    return words[1];
 }
 
 pafu_status pafu_workspace_counters(const void* ws, int64_t* counts, void* stream) {
@@ -713,6 +718,150 @@ pafu_status pafu_cache_update(pafu_cache* c, const pafu_head* head,
     }
     c->T += chunk;
     return PAFU_OK;
+}
+
+// ---- paged cache -----------------------------------------------------------------------------
+namespace {
+pafu_status paged_ok(const pafu_paged_cache* c) {
+    if (c == nullptr) return PAFU_ERR_INVALID_ARG;
+    if (c->n_heads < 1 || c->n_kv_heads < 1 || c->d_head < 1 || c->page_size < 1 || c->max_pages < 1 || c->n_requests < 0 || c->n_pages < 1)
+        return PAFU_ERR_INVALID_ARG;
+    if (c->type != PAFU_TYPE_BF16 && c->type != PAFU_TYPE_F16) return PAFU_ERR_INVALID_ARG;
+    if (c->cache_type != c->type && c->cache_type != PAFU_TYPE_E4M3) return PAFU_ERR_INVALID_ARG;
+    if (c->cache_type != PAFU_TYPE_E4M3 && (c->k_scale != nullptr || c->v_scale != nullptr)) return PAFU_ERR_INVALID_ARG;
+    if (c->n_heads % c->n_kv_heads != 0) return PAFU_ERR_INVALID_ARG;
+    if (c->d_head != 64 && c->d_head != 128) return PAFU_ERR_UNSUPPORTED_SHAPE;
+    if (c->n_heads > 65536) return PAFU_ERR_UNSUPPORTED_SHAPE;
+    if ((int64_t)c->page_size * c->max_pages > (1ll << 30)) return PAFU_ERR_UNSUPPORTED_SHAPE;
+    if (c->n_pages > 0x7fffffffLL || c->n_pages * (int64_t)c->page_size > 0x7fffffffLL) return PAFU_ERR_UNSUPPORTED_SHAPE;
+    const int64_t unit = 16 / type_bytes(c->cache_type);             // elements of 16 bytes
+    const int64_t strides[3] = {c->page_stride, c->token_stride, c->head_stride};
+    const int64_t counts[3] = {c->n_pages, c->page_size, c->n_kv_heads};
+    int64_t last = c->d_head;                                        // one past the last element
+    for (int i = 0; i < 3; ++i) {
+        if (counts[i] == 1) continue;                                // the stride of a single page, place or head is not used
+        if (strides[i] < 0 || strides[i] % unit != 0) return PAFU_ERR_INVALID_ARG;
+        if (strides[i] > (64ll << 30) / (counts[i] - 1)) return PAFU_ERR_UNSUPPORTED_SHAPE;
+        last += strides[i] * (counts[i] - 1);
+    }
+    if (last / unit > 0xffffffffLL) return PAFU_ERR_UNSUPPORTED_SHAPE;      // 32-bit addresses in 16-byte units
+    if (c->K == nullptr || c->V == nullptr || (c->n_requests > 0 && c->table == nullptr)) return PAFU_ERR_INVALID_ARG;
+    if (!aligned16(c->K) || !aligned16(c->V)) return PAFU_ERR_MISALIGNED;
+    if ((reinterpret_cast<uintptr_t>(c->table) & 3u) != 0 || (reinterpret_cast<uintptr_t>(c->k_scale) & 3u) != 0 ||
+        (reinterpret_cast<uintptr_t>(c->v_scale) & 3u) != 0) return PAFU_ERR_MISALIGNED;
+    return PAFU_OK;
+}
+
+// bytes from a pool's first to its last element
+size_t paged_pool_bytes(const pafu_paged_cache* c) {
+    int64_t last = c->d_head;
+    if (c->n_pages > 1) last += (c->n_pages - 1) * c->page_stride;
+    if (c->page_size > 1) last += (c->page_size - 1) * c->token_stride;
+    if (c->n_kv_heads > 1) last += (c->n_kv_heads - 1) * c->head_stride;
+    return (size_t)last * type_bytes(c->cache_type);
+}
+
+size_t paged_ws_bytes(const pafu_paged_cache* c) { return PAFU_PAGED_HEADER_BYTES + align_up(paged_part_bytes(c->d_head), 256); }
+
+pafu_status paged_ws_ok(const pafu_paged_cache* c, const void* ws, size_t ws_bytes) {
+    if (ws == nullptr) return PAFU_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(ws) & 255u) != 0) return PAFU_ERR_MISALIGNED;
+    return ws_bytes < paged_ws_bytes(c) ? PAFU_ERR_WORKSPACE_TOO_SMALL : PAFU_OK;
+}
+
+bool aligned_to(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+// rows [n0, n1] of d_head 16-bit elements with the given strides: whole 16-byte units, sizes that cannot wrap, and their extent in bytes
+pafu_status rows_ok(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t d_head, size_t* bytes) {
+    if (n0 == 1) s0 = 0;                                             // not used
+    if (n1 == 1) s1 = 0;
+    if (s0 < 0 || s1 < 0 || s0 % 8 != 0 || s1 % 8 != 0) return PAFU_ERR_INVALID_ARG;
+    if ((n0 > 1 && s0 > (1ll << 40) / (n0 - 1)) || (n1 > 1 && s1 > (1ll << 40) / (n1 - 1))) return PAFU_ERR_UNSUPPORTED_SHAPE;
+    *bytes = (size_t)((n0 - 1) * s0 + (n1 - 1) * s1 + d_head) * 2;
+    return PAFU_OK;
+}
+}  // namespace
+
+size_t pafu_paged_workspace_bytes(const pafu_paged_cache* cache) { return paged_ok(cache) == PAFU_OK ? paged_ws_bytes(cache) : 0; }
+
+pafu_status pafu_paged_tables(const pafu_paged_cache* c, const int32_t* len_old, const int32_t* len_new,
+                              int32_t* free_list, const int32_t* n_free, int32_t* n_free_out, int32_t* len_out,
+                              int64_t* slots, int64_t n_slots, int32_t* cu_new, void* ws, size_t ws_bytes, void* stream) {
+    pafu_status e = paged_ok(c);
+    if (e != PAFU_OK) return e;
+    if (n_slots < 0) return PAFU_ERR_INVALID_ARG;
+    if (n_slots > 0x7fffffffLL) return PAFU_ERR_UNSUPPORTED_SHAPE;
+    if (free_list == nullptr || n_free == nullptr || n_free_out == nullptr || cu_new == nullptr) return PAFU_ERR_INVALID_ARG;
+    if (n_slots > 0 && slots == nullptr) return PAFU_ERR_INVALID_ARG;
+    if (c->n_requests > 0 && (len_old == nullptr || len_new == nullptr || len_out == nullptr)) return PAFU_ERR_INVALID_ARG;
+    const void* words[] = {len_old, len_new, free_list, n_free, n_free_out, len_out, cu_new};
+    for (const void* p : words)
+        if (!aligned_to(p, 4)) return PAFU_ERR_MISALIGNED;
+    if (!aligned_to(slots, 8)) return PAFU_ERR_MISALIGNED;
+    {
+        // outputs overlap nothing, but for the updates in place
+        const size_t nR = (size_t)c->n_requests * 4;
+        struct { const void* p; size_t n; } out[] = {{c->table, nR * (size_t)c->max_pages}, {free_list, (size_t)c->n_pages * 4}, {n_free_out, 4},
+                                                     {len_out, nR}, {slots, (size_t)n_slots * 8}, {cu_new, nR + 4}},
+                                             in[] = {{len_old, nR}, {len_new, nR}, {n_free, 4}};
+        for (int i = 0; i < 6; ++i) {
+            for (int j = i + 1; j < 6; ++j)
+                if (ranges_overlap(out[i].p, out[i].n, out[j].p, out[j].n)) return PAFU_ERR_INVALID_ARG;
+            for (int j = 0; j < 3; ++j) {
+                const bool in_place = out[i].p == in[j].p && (i == 3 ? j < 2 : i == 2 && j == 2);
+                if (!in_place && ranges_overlap(out[i].p, out[i].n, in[j].p, in[j].n)) return PAFU_ERR_INVALID_ARG;
+            }
+        }
+    }
+    e = paged_ws_ok(c, ws, ws_bytes);
+    if (e != PAFU_OK) return e;
+    return launch_paged_tables(*c, len_old, len_new, free_list, n_free, n_free_out, len_out, slots, n_slots, cu_new, ws,
+                               static_cast<cudaStream_t>(stream));
+}
+
+pafu_status pafu_paged_append(const pafu_paged_cache* c, const void* Kn, const void* Vn, int64_t ld_token, int64_t ld_head,
+                              const int64_t* slots, int64_t n_tokens, void* ws, size_t ws_bytes, void* stream) {
+    pafu_status e = paged_ok(c);
+    if (e != PAFU_OK) return e;
+    if (n_tokens < 0) return PAFU_ERR_INVALID_ARG;
+    if (n_tokens == 0) return PAFU_OK;
+    if (n_tokens > 0x7fffffffLL / c->n_kv_heads) return PAFU_ERR_UNSUPPORTED_SHAPE;
+    if (Kn == nullptr || Vn == nullptr || slots == nullptr) return PAFU_ERR_INVALID_ARG;
+    size_t in_b = 0;
+    e = rows_ok(n_tokens, ld_token, c->n_kv_heads, ld_head, c->d_head, &in_b);
+    if (e != PAFU_OK) return e;
+    if (!aligned16(Kn) || !aligned16(Vn) || !aligned_to(slots, 8)) return PAFU_ERR_MISALIGNED;
+    const size_t pool_b = paged_pool_bytes(c);
+    if (ranges_overlap(Kn, in_b, c->K, pool_b) || ranges_overlap(Kn, in_b, c->V, pool_b) || ranges_overlap(Vn, in_b, c->K, pool_b) ||
+        ranges_overlap(Vn, in_b, c->V, pool_b)) return PAFU_ERR_INVALID_ARG;
+    e = paged_ws_ok(c, ws, ws_bytes);
+    if (e != PAFU_OK) return e;
+    return launch_paged_append(*c, Kn, Vn, ld_token, ld_head, slots, n_tokens, ws, static_cast<cudaStream_t>(stream));
+}
+
+pafu_status pafu_paged_attn(const pafu_paged_cache* c, const void* Q, int64_t q_token, int64_t q_head, const int32_t* lens,
+                            int64_t n_sink, int64_t n_recent, float scale, void* O, float* LSE,
+                            void* ws, size_t ws_bytes, void* stream) {
+    pafu_status e = paged_ok(c);
+    if (e != PAFU_OK) return e;
+    if (n_sink < 0) return PAFU_ERR_BAD_BUDGET;
+    if (!(scale >= 0.f) || isinf(scale)) return PAFU_ERR_INVALID_ARG;
+    if (c->n_requests == 0) return PAFU_OK;
+    if ((int64_t)c->n_requests * c->n_heads > 0x7fffffffLL) return PAFU_ERR_UNSUPPORTED_SHAPE;
+    if (Q == nullptr || lens == nullptr || O == nullptr) return PAFU_ERR_INVALID_ARG;
+    size_t q_b = 0;
+    e = rows_ok(c->n_requests, q_token, c->n_heads, q_head, c->d_head, &q_b);
+    if (e != PAFU_OK) return e;
+    if (!aligned16(Q) || !aligned16(O) || !aligned_to(lens, 4) || !aligned_to(LSE, 4)) return PAFU_ERR_MISALIGNED;
+    const size_t out_b = (size_t)c->n_requests * c->n_heads * c->d_head * 2, lse_b = LSE != nullptr ? (size_t)c->n_requests * c->n_heads * 4 : 0;
+    if (ranges_overlap(O, out_b, Q, q_b) || ranges_overlap(O, out_b, LSE, lse_b) || ranges_overlap(LSE, lse_b, Q, q_b)) return PAFU_ERR_INVALID_ARG;
+    const size_t pool_b = paged_pool_bytes(c);
+    if (ranges_overlap(O, out_b, c->K, pool_b) || ranges_overlap(O, out_b, c->V, pool_b) || ranges_overlap(LSE, lse_b, c->K, pool_b) ||
+        ranges_overlap(LSE, lse_b, c->V, pool_b)) return PAFU_ERR_INVALID_ARG;
+    e = paged_ws_ok(c, ws, ws_bytes);
+    if (e != PAFU_OK) return e;
+    if (scale == 0.f) scale = 1.0f / sqrtf((float)c->d_head);
+    return launch_paged_attn(*c, Q, q_token, q_head, lens, n_sink, n_recent, scale, O, LSE, ws, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

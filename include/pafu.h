@@ -419,7 +419,7 @@ typedef struct pafu_paged_cache {
  * 256-byte aligned.  It serves caches of the same d_head and any other geometry (0 = invalid cache), one call at a time: calls that may
  * overlap on the GPU - two streams, two captured graphs that run side by side - need a workspace each.  It is not for the
  * calls above: what those leave behind the header would be taken for counters. */
-#define PAFU_PAGED_HEADER_BYTES 4608
+#define PAFU_PAGED_HEADER_BYTES 12800
 size_t pafu_paged_workspace_bytes(const pafu_paged_cache* cache);
 
 /* Block tables and slot map of a step, from the requests' lengths.  With P(x) = ceil(x / page_size):
@@ -464,8 +464,8 @@ pafu_status pafu_paged_append(const pafu_paged_cache* cache, const void* Kn, con
  * own key and value are among them once pafu_paged_append has written them and lens counts them.
  * n_recent < 0 keeps every position; otherwise the n_sink first and the n_recent last ones (the attention-sink prefix and the recent
  * window of pafu_policy) are kept.  Positions outside are not read, whatever they hold.
- * fp32 accumulation and softmax; the probabilities enter the product as 16-bit values, with what that rounding leaves over
- * as a second term for bf16 pools and wherever G % 16 is in 1..8 or G <= 8.
+ * fp32 accumulation and softmax; the probabilities enter the product as 16-bit values of the pools' type (fp16 for e4m3), for
+ * bf16 followed by what that rounding leaves over.
  *   Q         device [n_requests, n_heads, d_head] of cache->type with strides q_token and q_head in elements (multiples of 8), 16-byte
  *             aligned
  *   lens      device int32 [n_requests]

@@ -6,11 +6,12 @@ namespace pafu {
 
 // Workspace of the paged entry points: status header (256 bytes), tickets (zero between calls), partial results.
 constexpr int kStatusWordPaged = 1;            // a pafu_status that a kernel of the paged cache found on the device
-constexpr int kPagedTickets = 1088;            // 32-bit words behind the header: one a CTA of the attention, the last one the tables' own
+constexpr int kPaTicketRow = 1024;             // CTAs of the attention kernel, at most
+constexpr int kPagedTickets = 3 * kPaTicketRow + 64;      // 32-bit words behind the header: three a CTA of the attention, the last one the tables' own
 constexpr size_t kPagedPartOffset = kWsHeaderBytes + kPagedTickets * 4;
 constexpr int kPagedCtasPerSm = 4;             // most CTAs of the attention kernel on an SM
 constexpr int kPagedRows = 16;                 // query heads that one item handles (rows of a tensor-core tile)
-static_assert(kPagedCtasPerSm * kMaxPersistentGrid < kPagedTickets, "a ticket for every CTA");
+static_assert(kPagedCtasPerSm * kMaxPersistentGrid <= kPaTicketRow, "a ticket for every CTA");
 static_assert(kPagedPartOffset % 256 == 0 && kPagedPartOffset == PAFU_PAGED_HEADER_BYTES, "the part of the workspace that starts at zero");
 
 // n / d for 0 <= n < 2^31 as a product: m = floor(2^(31+s) / d) + 1 with s = ceil(log2 d) has an excess below

@@ -3,22 +3,26 @@
 //
 // Every key is used by the n_heads / n_kv_heads query heads of its group, 2 flop a byte and head: the cache's bytes bound
 // the call, and what a kernel has to do is keep enough of them on their way.  So nothing is staged: a warp's lanes load
-// 16-byte pieces of the rows straight into the registers in which mma.sync wants them.  The order of the contraction
-// index is free as long as both operands follow it, so a lane's 16 contiguous bytes of a key row serve as two (8 bits: four)
-// B fragments of Q K^T, and the queries are loaded in the same order; the columns of P V are free too, so eight
-// neighbouring lanes read a 128-byte line of a value row and a byte permute pairs the rows of two keys.  The rows' addresses
-// come from the page table one tile ahead, so pages of any length, order and stride cost the same and may end inside a tile.
-// Up to eight query heads fill half of the 16 rows of a product's tile; the other half then carries what rounding the
-// probabilities to 16 bits leaves over, which makes P V nearly exact at no cost.  With 9 to 16 heads a second product does
-// that for bf16; fp16 probabilities (2^-12) need none.
+// 16-byte pieces of the rows straight into the registers in which mma.sync wants them.  Keys are the rows of S^T = K Q^T and
+// the d_head components the rows of O^T = V^T P^T, heads the columns, eight a product: the accumulators of O^T then take half the registers
+// that O with 16 rows for at most eight heads would.  The order of the contraction index is free as long as both
+// operands follow it, so a lane's 16 contiguous bytes of a key row serve as parts of two (8 bits: four) fragments, and the
+// queries are loaded in the same order; the order of O^T's rows is free too, so eight neighbouring lanes read a 128-byte line of a
+// value row and a byte permute pairs the rows of two keys.  P goes from S^T's layout to the other product's by 8 x 8 transposes
+// in registers.  The rows' addresses come from the page table one tile ahead, so pages of any length, order and
+// stride cost the same and may end inside a tile.
+// Probabilities enter the product as 16-bit values.  For bf16 what that rounding leaves over follows in a second product
+// (2^-17 of a probability is lost then); fp16 keeps 2^-12, half a step of an fp16 output.
 // 8-bit caches are widened to fp16, which holds every e4m3 value; bf16 queries are scaled by a power of two a row so that
 // their largest component lies in [2^14, 2^15) and fp16 holds them to 2^-39 of it.
 //
 // Split over the length: every (request, group of heads) is an item of ceil(kept / step) steps (a step is one tile for each of
 // the four warps) and a fixed cost.  All items laid end to end are cut into equal shares, one a CTA, by arithmetic that every
 // CTA does for itself from the lengths on the device: the grid does not depend on the lengths, and a captured launch follows
-// them.  A share's first and last item may continue in other CTAs: their fp32 partial results go to the workspace,
-// and the CTA that arrives last (a counter; nothing waits) joins them in a fixed order, so results do not depend on timing.
+// them.  A cut that would leave less than a few steps of an item on one side moves to the item's end.  A share's first and last
+// item may continue in other CTAs: their fp32 partial results go to the workspace, and the CTA that arrives last
+// (a counter; nothing waits) joins them in a fixed order, so results do not depend on timing; more than 16 pieces are joined
+// in groups of 16 first, by as many CTAs.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math.h>
@@ -33,6 +37,9 @@ constexpr int kPaWarps = 4;
 constexpr int kPaThreads = kPaWarps * 32;
 constexpr int kPaItemCost = 1;        // what an item costs beside its steps, in steps
 constexpr int kPaMinShare = 4;        // steps and item costs that a CTA takes at least
+constexpr int kPaSnap = 4;            // a cut this near to an item's end moves there
+constexpr int kPaJoin = 16;           // pieces that are joined at once
+static_assert(3 * kPaTicketRow < kPagedTickets, "three counters a CTA, and the tables' own");
 
 struct PagedAttnArgs {
     PagedPool pool;
@@ -57,20 +64,22 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 
-// 16 bytes (8) of a row, or zeros
+// 16 (8) bytes of a row
+__device__ __forceinline__ void ld_row(uint32_t (&w)[4], const char* p) {
+    asm volatile("ld.global.nc.L1::no_allocate.L2::128B.v4.u32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p) : "memory");
+}
+__device__ __forceinline__ void ld_row(uint32_t (&w)[2], const char* p) {
+    asm volatile("ld.global.nc.L1::no_allocate.L2::128B.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p) : "memory");
+}
+// the same, or zeros
 __device__ __forceinline__ void ld_row(uint32_t (&w)[4], const char* p, bool ok) {
     w[0] = w[1] = w[2] = w[3] = 0u;
-    asm volatile(
-        "{\n\t.reg .pred P;\n\tsetp.ne.b32 P, %5, 0;\n\t"
-        "@P ld.global.nc.L1::no_allocate.L2::128B.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
-        : "+r"(w[0]), "+r"(w[1]), "+r"(w[2]), "+r"(w[3]) : "l"(p), "r"((int)ok) : "memory");
+    if (ok) ld_row(w, p);
 }
 __device__ __forceinline__ void ld_row(uint32_t (&w)[2], const char* p, bool ok) {
     w[0] = w[1] = 0u;
-    asm volatile(
-        "{\n\t.reg .pred P;\n\tsetp.ne.b32 P, %3, 0;\n\t"
-        "@P ld.global.nc.L1::no_allocate.L2::128B.v2.u32 {%0, %1}, [%2];\n\t}"
-        : "+r"(w[0]), "+r"(w[1]) : "l"(p), "r"((int)ok) : "memory");
+    if (ok) ld_row(w, p);
 }
 
 template <bool F16>
@@ -81,6 +90,13 @@ __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uin
     else
         asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
             : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// an 8 x 8 matrix of 16-bit values, a row of four lanes' pairs each, transposed
+__device__ __forceinline__ uint32_t transpose8(uint32_t v) {
+    uint32_t r;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
 }
 
 // two fp32 values as a pair of 16-bit ones, the first in the low half
@@ -99,11 +115,10 @@ __device__ __forceinline__ float2 unpack2(uint32_t v) {
     return __bfloat1622float2(*reinterpret_cast<__nv_bfloat162*>(&v));
 }
 
-// two e4m3 values (a 16-bit pair) as two fp16 ones
-__device__ __forceinline__ uint32_t widen2(uint32_t pair) {
-    uint32_t r;
-    asm("{\n\t.reg .b16 h;\n\tcvt.u16.u32 h, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, h;\n\t}" : "=r"(r) : "r"(pair));
-    return r;
+// four e4m3 values as two pairs of fp16 ones
+__device__ __forceinline__ void widen4(uint32_t w, uint32_t& lo, uint32_t& hi) {
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
+        : "=r"(lo), "=r"(hi) : "r"(w));
 }
 
 // Position of the kept keys of a request and their number.
@@ -134,12 +149,15 @@ struct Tile {
     static constexpr int VB = D * ES / 8 < 16 ? 8 : 16;           // bytes of a value load
     static constexpr int VC = D * ES / 8 / VB;                    // loads a value row
     static constexpr int VE = VB / ES;                            // elements of a value load
-    static constexpr int NT = D / 8;                              // column tiles of O
+    static constexpr int NT = D / 16;                             // row tiles of O^T
     static constexpr int STEP = KT * kPaWarps;
     static constexpr bool F16 = F16Q || E4M3;                     // type of the products
     static constexpr int ROWS = HG * 8;
     static constexpr int LD = D + 4;
+    static constexpr int CTAS = HG * D <= 128 ? 3 : 2;            // an SM: 168 or 255 registers a thread
     static constexpr size_t SMEM = sizeof(float) * (kPaWarps * ROWS * LD + 2 * kPaWarps * ROWS);
+    static_assert(KT % 16 == 0 && VE % 4 == 0, "fragments");
+    static_assert(2 * kPaJoin * kPagedRows <= kPaWarps * ROWS * LD, "the pieces' maxima and sums fit where the warps' results were");
 };
 
 // Address of a key: its row of the pools in 16-byte units (head included), or ~0
@@ -166,27 +184,102 @@ __device__ __forceinline__ uint32_t key_offset(const PagedAttnArgs& a, const Key
     return (uint32_t)x.page * a.pool.page_u + x.in_page;
 }
 
+// Where a CTA begins or ends: a position on the line of all items, and the request and item it lies in.
+struct Cut {
+    int64_t at, item_at;      // the position; where its item begins
+    int32_t r, item;
+};
+
+// Where an item's heads go, and how
+template <int D, bool F16Q>
+struct Rows {
+    char* O;
+    float* LSE;
+    int32_t lse_stride;
+    float v_scale;
+    __device__ void store(int row, int d, const float (&x)[4], float top, float sum) const {
+        const float inv = sum == 0.f ? 0.f : v_scale / sum;
+        uint2 w;
+        w.x = pack2<F16Q>(x[0] * inv, x[1] * inv);
+        w.y = pack2<F16Q>(x[2] * inv, x[3] * inv);
+        *reinterpret_cast<uint2*>(O + ((int64_t)row * D + d) * 2) = w;
+        if (LSE != nullptr && d == 0) LSE[(int64_t)row * lse_stride] = top * 0.6931471805599453f + logf(sum);
+    }
+};
+// A piece's results in the workspace: numerators, maxima, sums
+template <int D>
+constexpr size_t kPartWords = (size_t)kPagedRows * (D + 2);
+template <int D>
+__device__ __forceinline__ void put_part(float* part, int row, int d, const float (&x)[4], float top, float sum) {
+    *reinterpret_cast<float4*>(part + row * D + d) = make_float4(x[0], x[1], x[2], x[3]);
+    if (d == 0) {
+        part[kPagedRows * D + row] = top;
+        part[kPagedRows * D + kPagedRows + row] = sum;
+    }
+}
+
+// Pieces p0, p0 + by, ... (count <= kPaJoin) of the item whose first piece is CTA `first`'s, joined by the whole CTA: to the output, or in
+// place of piece p0.  A call, so that its registers do not count in the loop over the keys.
+template <int D, bool F16Q>
+__device__ __noinline__ void join_pieces(float* parts, int first, int p0, int by, int count, int rows, float* shared, const Rows<D, F16Q>* out) {
+    constexpr int PER = 4, COLS = D / PER;
+    const int tid = threadIdx.x;
+    float* jm = shared;                                      // [piece][row]
+    float* jl = shared + kPaJoin * kPagedRows;
+    auto piece = [&](int i) { const int p = p0 + i * by; return parts + (2 * (size_t)(first + p) + (p == 0)) * kPartWords<D>; };
+    __syncthreads();
+    for (int i = tid; i < count * kPagedRows; i += kPaThreads) {
+        const float* q = piece(i / kPagedRows) + kPagedRows * D + i % kPagedRows;
+        if (i % kPagedRows < rows) jm[i] = __ldcg(q), jl[i] = __ldcg(q + kPagedRows);
+    }
+    __syncthreads();
+    for (int i = tid; i < rows * COLS; i += kPaThreads) {
+        const int row = i / COLS, d = i % COLS * PER;
+        float4 y[kPaJoin];
+#pragma unroll
+        for (int p = 0; p < kPaJoin; ++p) y[p] = p < count ? __ldcg(reinterpret_cast<const float4*>(piece(p) + row * D + d)) : make_float4(0.f, 0.f, 0.f, 0.f);
+        float top = -INFINITY;
+        for (int p = 0; p < count; ++p) top = fmaxf(top, jm[p * kPagedRows + row]);
+        const float base = top == -INFINITY ? 0.f : top;
+        float x[PER] = {0.f, 0.f, 0.f, 0.f}, sum = 0.f;
+#pragma unroll
+        for (int p = 0; p < kPaJoin; ++p)
+            if (p < count) {
+                const float f = ex2(jm[p * kPagedRows + row] - base);
+                sum += f * jl[p * kPagedRows + row];
+                x[0] += f * y[p].x, x[1] += f * y[p].y, x[2] += f * y[p].z, x[3] += f * y[p].w;
+            }
+        if (out != nullptr) out->store(row, d, x, top, sum);
+        else put_part<D>(piece(0), row, d, x, top, sum);
+    }
+    __syncthreads();
+}
+
 template <int D, bool F16Q, bool E4M3, int HG>
-__global__ void __launch_bounds__(kPaThreads, HG == 1 ? 3 : 2) paged_attn_kernel(const PagedAttnArgs a) {
+__global__ void __launch_bounds__(kPaThreads, (Tile<D, F16Q, E4M3, HG>::CTAS)) paged_attn_kernel(const PagedAttnArgs a) {
     using C = Tile<D, F16Q, E4M3, HG>;
     extern __shared__ __align__(16) float sm[];
     float* sO = sm;                                   // [warp][row][LD]
     float* sM = sm + kPaWarps * C::ROWS * C::LD;      // [warp][row]
     float* sL = sM + kPaWarps * C::ROWS;
-    __shared__ int64_t plan_sum[kPaWarps], plan_at;
-    __shared__ int32_t plan_r, last_flag;
+    __shared__ int64_t plan_sum[kPaWarps];
+    __shared__ Cut cuts[2];
+    __shared__ int32_t last_flag;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     const int H = a.n_kv * a.parts;                   // items a request
 
     grid_dep_wait();
 
     // ---- this CTA's share of all steps
-    int64_t share, begin;
+    auto kept_at = [&](int r) { return kept_of(a, ld_index(a.lens + r)); };
+    auto steps_of = [](const Kept& k) { return max((k.n + C::STEP - 1) / C::STEP, 1); };
+    int64_t share;
+    int snap;
     {
         const int per = (a.n_requests + kPaThreads - 1) / kPaThreads;
         const int r0 = min(tid * per, a.n_requests), r1 = min(r0 + per, a.n_requests);
         int64_t mine = 0;
-        for (int r = r0; r < r1; ++r) mine += max((kept_of(a, ld_index(a.lens + r)).n + C::STEP - 1) / C::STEP, 1) + kPaItemCost;
+        for (int r = r0; r < r1; ++r) mine += steps_of(kept_at(r)) + kPaItemCost;
         int64_t inc = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -202,330 +295,383 @@ __global__ void __launch_bounds__(kPaThreads, HG == 1 ? 3 : 2) paged_attn_kernel
         }
         all *= H;
         before *= H;
-        share = (all + gridDim.x - 1) / gridDim.x;
-        if (share < kPaMinShare) share = kPaMinShare;
-        begin = share * blockIdx.x;
-        if (begin >= all) return;
-        if (begin >= before && begin < before + mine * H) {
-            int64_t at = before;
-            int r = r0;
-            for (; r < r1; ++r) {
-                const int64_t c = (int64_t)H * (max((kept_of(a, ld_index(a.lens + r)).n + C::STEP - 1) / C::STEP, 1) + kPaItemCost);
-                if (begin < at + c) break;
-                at += c;
+        share = max((all + gridDim.x - 1) / gridDim.x, (int64_t)kPaMinShare);
+        snap = (int)min(share / 2, (int64_t)kPaSnap);
+        if (share * blockIdx.x >= all) return;
+        for (int i = 0; i < 2; ++i) {
+            const int64_t b = share * (blockIdx.x + i);
+            if (b >= all) {
+                if (tid == 0) cuts[i] = Cut{all, all, a.n_requests, 0};
+            } else if (b >= before && b < before + mine * H) {
+                int64_t at = before;
+                int r = r0, cost = 0;
+                for (; r < r1; ++r) {
+                    cost = steps_of(kept_at(r)) + kPaItemCost;
+                    if (b < at + (int64_t)H * cost) break;
+                    at += (int64_t)H * cost;
+                }
+                Cut c;
+                c.r = r;
+                c.item = (int)((b - at) / cost);
+                c.item_at = at + (int64_t)c.item * cost;
+                const int o = (int)(b - c.item_at);
+                c.at = o < snap ? c.item_at : b;
+                if (o >= snap && cost - o <= snap) {             // on to the next item
+                    c.item_at += cost;
+                    c.at = c.item_at;
+                    if (++c.item == H) c.item = 0, ++c.r;
+                }
+                cuts[i] = c;
             }
-            plan_r = r;
-            plan_at = at;
         }
         __syncthreads();
     }
-    const int64_t end = begin + share;
-    int r = plan_r;
-    Kept kept = kept_of(a, ld_index(a.lens + r));
-    int steps = max((kept.n + C::STEP - 1) / C::STEP, 1);
-    int item = (int)((begin - plan_at) / (steps + kPaItemCost));
-    int64_t at = plan_at + (int64_t)item * (steps + kPaItemCost);     // where the item starts
+    const int64_t begin = cuts[0].at, end = cuts[1].at;
+    if (begin >= end) return;
+    int r = cuts[0].r, item = cuts[0].item;
+    int64_t at = cuts[0].item_at;                     // where the item starts
+    Kept kept = kept_at(r);
 
     while (true) {
-        const int lo = (int)min((int64_t)steps, max(begin - at, (int64_t)0));
+        const int steps = steps_of(kept), cost = steps + kPaItemCost;
+        const int lo = (int)max(begin - at, (int64_t)0);
         const int hi = (int)min((int64_t)steps, end - at);
-        const bool whole = lo == 0 && hi == steps;
-        if (lo < hi) {
-            const int kv = item / a.parts, head0 = kv * a.group + (item - kv * a.parts) * kPagedRows;
-            const int rows = min(kPagedRows, (kv + 1) * a.group - head0);       // query heads of the item
-            const int32_t* table = a.pool.table + (int64_t)r * a.pool.max_pages;
-            const uint32_t head_u = (uint32_t)kv * a.pool.head_u;
+        const int kv = item / a.parts, head0 = kv * a.group + (item - kv * a.parts) * kPagedRows;
+        const int rows = min(kPagedRows, (kv + 1) * a.group - head0);       // query heads of the item
+        const int32_t* table = a.pool.table + (int64_t)r * a.pool.max_pages;
+        const uint32_t head_u = (uint32_t)kv * a.pool.head_u;
 
-            uint32_t K[C::KR][C::KW / 4][4], V[C::VR][C::VC][C::VB / 4];
-            auto load_K = [&](uint32_t off) {
+        uint32_t K[C::KR][C::KW / 4][4], V[C::VR][C::VC][C::VB / 4];
+        auto load_K = [&](uint32_t off, bool full) {
 #pragma unroll
-                for (int i = 0; i < C::KR; ++i) {
-                    const uint32_t o = __shfl_sync(0xffffffffu, off, i * 8 + g);
-                    const char* p = a.pool.K + (uint64_t)o * 16 + t * 16;
-#pragma unroll
-                    for (int c = 0; c < C::KW / 4; ++c) ld_row(K[i][c], p + c * 64, o != ~0u);
-                }
-            };
-            auto load_V = [&](uint32_t off) {
-#pragma unroll
-                for (int i = 0; i < C::VR; ++i) {
-                    const uint32_t o = __shfl_sync(0xffffffffu, off, (i >> 2) * 16 + ((i >> 1) & 1) * 8 + 2 * t + (i & 1));
-                    const char* p = a.pool.V + (uint64_t)o * 16 + g * C::VB;
-#pragma unroll
-                    for (int c = 0; c < C::VC; ++c) ld_row(V[i][c], p + c * 8 * C::VB, o != ~0u);
-                }
-            };
-
-            // the first tile's rows are requested before the queries
-            int32_t j = (lo * kPaWarps + warp) * C::KT + (lane & (C::KT - 1));
-            const int32_t j_end = hi * C::STEP;           // exclusive; keys past kept.n do not exist
-            auto ask = [&](int32_t jj) { return key_at(a, kept, table, jj < j_end ? jj : 0x7fffffff, head_u); };
-            uint32_t off = key_offset(a, ask(j));
-            KeyAt next = ask(j + C::STEP);
-            load_K(off);
-            load_V(off);
-
-            // queries: rows g (and g + 8), in the order in which the lane's key words come
-            uint32_t qf[HG][D / 16][2];
-            float c_row[HG];
-#pragma unroll
-            for (int hg = 0; hg < HG; ++hg) {
-                const bool have = hg * 8 + g < rows;
-                const char* qp = a.Q + r * a.q_token + (int64_t)(head0 + hg * 8 + g) * a.q_head;
+            for (int i = 0; i < C::KR; ++i) {
+                const uint32_t o = __shfl_sync(0xffffffffu, off, i * 8 + g);
+                const char* p = a.pool.K + (uint64_t)o * 16 + t * 16;
 #pragma unroll
                 for (int c = 0; c < C::KW / 4; ++c) {
-                    // elements of 16 bytes of a key row: 8 or 16
-                    constexpr int PER = 16 / C::ES;
-                    const char* p = qp + (c * 4 * PER + t * PER) * 2;
-#pragma unroll
-                    for (int h = 0; h < PER / 8; ++h) {
-                        uint4 w = make_uint4(0, 0, 0, 0);
-                        if (have) w = *reinterpret_cast<const uint4*>(p + h * 16);
-                        const int ks = c * (PER / 4) + h * 2;
-                        qf[hg][ks][0] = w.x;
-                        qf[hg][ks][1] = w.y;
-                        qf[hg][ks + 1][0] = w.z;
-                        qf[hg][ks + 1][1] = w.w;
-                    }
-                }
-                c_row[hg] = a.scale;
-                if (E4M3 && a.k_scale != nullptr) c_row[hg] *= a.k_scale[kv];
-                if (E4M3 && !F16Q) {
-                    float top = 0.f;
-#pragma unroll
-                    for (int ks = 0; ks < D / 16; ++ks)
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const float2 v = unpack2<false>(qf[hg][ks][i]);
-                            top = fmaxf(top, fmaxf(fabsf(v.x), fabsf(v.y)));
-                        }
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                    // 2^(14 - e) with e the exponent of the largest component; rows of zeros or with infinities stay
-                    const int e = (int)(__float_as_uint(top) >> 23);
-                    const int up = e == 0 || e == 255 ? 0 : min(14 + 127 - e, 100);
-                    const float f = __uint_as_float((uint32_t)(up + 127) << 23);
-                    c_row[hg] *= __uint_as_float((uint32_t)(127 - up) << 23);
-#pragma unroll
-                    for (int ks = 0; ks < D / 16; ++ks)
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const float2 v = unpack2<false>(qf[hg][ks][i]);
-                            qf[hg][ks][i] = pack2<true>(v.x * f, v.y * f);
-                        }
+                    if (full) ld_row(K[i][c], p + c * 64);
+                    else ld_row(K[i][c], p + c * 64, o != ~0u);
                 }
             }
-
-            float o[C::NT][4];
-            float m[HG], l[HG];
+        };
+        auto load_V = [&](uint32_t off, bool full) {
 #pragma unroll
-            for (int n = 0; n < C::NT; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
+            for (int i = 0; i < C::VR; ++i) {
+                const uint32_t o = __shfl_sync(0xffffffffu, off, (i >> 2) * 16 + ((i >> 1) & 1) * 8 + 2 * t + (i & 1));
+                const char* p = a.pool.V + (uint64_t)o * 16 + g * C::VB;
 #pragma unroll
-            for (int hg = 0; hg < HG; ++hg) m[hg] = -INFINITY, l[hg] = 0.f;
-
-            for (int s = lo; s < hi; ++s) {
-                const uint32_t valid = __ballot_sync(0xffffffffu, off != ~0u) & (C::KT == 32 ? ~0u : (1u << C::KT % 32) - 1u);
-                const uint32_t off_next = key_offset(a, next);
-                j += C::STEP;
-                next = ask(j + C::STEP);
-                // S = Q K^T: rows are heads, columns keys
-                float S[C::KR][4];
-#pragma unroll
-                for (int i = 0; i < C::KR; ++i) {
-                    S[i][0] = S[i][1] = S[i][2] = S[i][3] = 0.f;
-#pragma unroll
-                    for (int ks = 0; ks < D / 16; ++ks) {
-                        uint32_t b0, b1;
-                        if (E4M3) {
-                            const uint32_t w = K[i][ks / 4][ks % 4];
-                            b0 = widen2(w & 0xffffu);
-                            b1 = widen2(w >> 16);
-                        } else {
-                            b0 = K[i][ks / 2][ks % 2 * 2];
-                            b1 = K[i][ks / 2][ks % 2 * 2 + 1];
-                        }
-                        mma<C::F16>(S[i], qf[0][ks][0], HG == 2 ? qf[HG - 1][ks][0] : 0u, qf[0][ks][1], HG == 2 ? qf[HG - 1][ks][1] : 0u, b0, b1);
-                    }
+                for (int c = 0; c < C::VC; ++c) {
+                    if (full) ld_row(V[i][c], p + c * 8 * C::VB);
+                    else ld_row(V[i][c], p + c * 8 * C::VB, o != ~0u);
                 }
-                if (s + 1 < hi) load_K(off_next);
+            }
+        };
+        auto valid_of = [](uint32_t off) {
+            return __ballot_sync(0xffffffffu, off != ~0u) & (C::KT == 32 ? ~0u : (1u << C::KT % 32) - 1u);
+        };
+        constexpr uint32_t kFull = C::KT == 32 ? ~0u : (1u << C::KT % 32) - 1u;
 
-                // running maximum and sum, one or two rows a lane, shared by the four lanes of a row
-                uint32_t ph[C::KR][HG], pl[C::KR][HG];
-                float f[HG];
-                bool moved = false;
+        // the first tile's rows are requested before the queries
+        int32_t j = (lo * kPaWarps + warp) * C::KT + (lane & (C::KT - 1));
+        const int32_t j_end = hi * C::STEP;           // exclusive; keys past kept.n do not exist
+        auto ask = [&](int32_t jj) { return key_at(a, kept, table, jj < j_end ? jj : 0x7fffffff, head_u); };
+        uint32_t off = key_offset(a, ask(j));
+        KeyAt next = ask(j + C::STEP);
+        uint32_t valid = valid_of(off);
+        load_K(off, valid == kFull);
+        load_V(off, valid == kFull);
+
+        // queries: head g (and g + 8), in the order in which the lane's key words come
+        uint32_t qf[HG][D / 16][2];
+        float c_col[HG][2];                           // factor of the logits of heads 2t, 2t + 1
 #pragma unroll
-                for (int hg = 0; hg < HG; ++hg) {
-                    float top = -INFINITY;
+        for (int hg = 0; hg < HG; ++hg) {
+            const bool have = hg * 8 + g < rows;
+            const char* qp = a.Q + r * a.q_token + (int64_t)(head0 + hg * 8 + g) * a.q_head;
 #pragma unroll
-                    for (int i = 0; i < C::KR; ++i)
+            for (int c = 0; c < C::KW / 4; ++c) {
+                constexpr int PER = 16 / C::ES;       // elements of 16 bytes of a key row
+                const char* p = qp + (c * 4 * PER + t * PER) * 2;
 #pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            float x = S[i][hg * 2 + k] * c_row[hg];
-                            if (!(valid >> (i * 8 + 2 * t + k) & 1u)) x = -INFINITY;
-                            S[i][hg * 2 + k] = x;
-                            top = fmaxf(top, x);
+                for (int h = 0; h < PER / 8; ++h) {
+                    uint4 w = make_uint4(0, 0, 0, 0);
+                    if (have) w = *reinterpret_cast<const uint4*>(p + h * 16);
+                    const int ks = c * (PER / 4) + h * 2;
+                    qf[hg][ks][0] = w.x;
+                    qf[hg][ks][1] = w.y;
+                    qf[hg][ks + 1][0] = w.z;
+                    qf[hg][ks + 1][1] = w.w;
+                }
+            }
+            float c_row = a.scale;
+            if (E4M3 && a.k_scale != nullptr) c_row *= a.k_scale[kv];
+            if (E4M3 && !F16Q) {
+                float top = 0.f;
+#pragma unroll
+                for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const float2 v = unpack2<false>(qf[hg][ks][i]);
+                        top = fmaxf(top, fmaxf(fabsf(v.x), fabsf(v.y)));
+                    }
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                // 2^(14 - e) with e the exponent of the largest component; rows of zeros or with infinities stay
+                const int e = (int)(__float_as_uint(top) >> 23);
+                const int up = e == 0 || e == 255 ? 0 : min(14 + 127 - e, 100);
+                const float f = __uint_as_float((uint32_t)(up + 127) << 23);
+                c_row *= __uint_as_float((uint32_t)(127 - up) << 23);
+#pragma unroll
+                for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const float2 v = unpack2<false>(qf[hg][ks][i]);
+                        qf[hg][ks][i] = pack2<true>(v.x * f, v.y * f);
+                    }
+            }
+            c_col[hg][0] = __shfl_sync(0xffffffffu, c_row, 8 * t);
+            c_col[hg][1] = __shfl_sync(0xffffffffu, c_row, 8 * t + 4);
+        }
+
+        float o[C::NT][HG][4];
+        float m[HG][2], l[HG][2];                     // of heads 2t and 2t + 1; l of this lane's keys
+#pragma unroll
+        for (int n = 0; n < C::NT; ++n)
+#pragma unroll
+            for (int hg = 0; hg < HG; ++hg) o[n][hg][0] = o[n][hg][1] = o[n][hg][2] = o[n][hg][3] = 0.f;
+#pragma unroll
+        for (int hg = 0; hg < HG; ++hg) m[hg][0] = m[hg][1] = -INFINITY, l[hg][0] = l[hg][1] = 0.f;
+
+        for (int s = lo; s < hi; ++s) {
+            const uint32_t off_next = key_offset(a, next);
+            j += C::STEP;
+            next = ask(j + C::STEP);
+            const uint32_t valid_next = valid_of(off_next);
+            const bool more = s + 1 < hi;
+            if (valid == 0u) {                        // a short item: nothing for this warp
+                if (more) {
+                    load_K(off_next, false);
+                    load_V(off_next, false);
+                }
+                valid = valid_next;
+                continue;
+            }
+            // S^T = K Q^T: rows are keys, columns heads
+            float S[C::KT / 16][HG][4];
+#pragma unroll
+            for (int i = 0; i < C::KT / 16; ++i) {
+#pragma unroll
+                for (int hg = 0; hg < HG; ++hg) S[i][hg][0] = S[i][hg][1] = S[i][hg][2] = S[i][hg][3] = 0.f;
+#pragma unroll
+                for (int ks = 0; ks < D / 16; ++ks) {
+                    uint32_t a0, a1, a2, a3;
+                    if (E4M3) {
+                        widen4(K[2 * i][ks / 4][ks % 4], a0, a2);
+                        widen4(K[2 * i + 1][ks / 4][ks % 4], a1, a3);
+                    } else {
+                        a0 = K[2 * i][ks / 2][ks % 2 * 2];
+                        a1 = K[2 * i + 1][ks / 2][ks % 2 * 2];
+                        a2 = K[2 * i][ks / 2][ks % 2 * 2 + 1];
+                        a3 = K[2 * i + 1][ks / 2][ks % 2 * 2 + 1];
+                    }
+#pragma unroll
+                    for (int hg = 0; hg < HG; ++hg) mma<C::F16>(S[i][hg], a0, a1, a2, a3, qf[hg][ks][0], qf[hg][ks][1]);
+                }
+            }
+            if (more) load_K(off_next, valid_next == kFull);
+
+            // running maximum and sum of two heads (four for 16) a lane
+#pragma unroll
+            for (int i = 0; i < C::KT / 16; ++i)
+#pragma unroll
+                for (int hg = 0; hg < HG; ++hg)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) S[i][hg][k] *= c_col[hg][k & 1];
+            if (valid != kFull) {
+#pragma unroll
+                for (int i = 0; i < C::KT / 16; ++i)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (!(valid >> (i * 16 + (k >> 1) * 8 + g) & 1u)) {
+#pragma unroll
+                            for (int hg = 0; hg < HG; ++hg) S[i][hg][k] = -INFINITY;
                         }
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                    const float now = fmaxf(m[hg], top);
-                    const float base = now == -INFINITY ? 0.f : now;
-                    f[hg] = ex2(m[hg] - base);
-                    moved |= now != m[hg];
-                    m[hg] = now;
+            }
+            float f[HG][2];
+            bool moved = false;
+#pragma unroll
+            for (int hg = 0; hg < HG; ++hg)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    float top = m[hg][k];
+#pragma unroll
+                    for (int i = 0; i < C::KT / 16; ++i) top = fmaxf(top, fmaxf(S[i][hg][k], S[i][hg][k + 2]));
+                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+                    const float base = top == -INFINITY ? 0.f : top;
+                    f[hg][k] = ex2(m[hg][k] - base);
+                    moved |= top != m[hg][k];
+                    m[hg][k] = top;
                     float sum = 0.f;
 #pragma unroll
-                    for (int i = 0; i < C::KR; ++i) {
-                        const float x = ex2(S[i][hg * 2] - base), y = ex2(S[i][hg * 2 + 1] - base);
-                        sum += x + y;
-                        ph[i][hg] = pack2<C::F16>(x, y);
-                        const float2 back = unpack2<C::F16>(ph[i][hg]);
-                        pl[i][hg] = pack2<C::F16>(x - back.x, y - back.y);
+                    for (int i = 0; i < C::KT / 16; ++i) {
+                        S[i][hg][k] = ex2(S[i][hg][k] - base);
+                        S[i][hg][k + 2] = ex2(S[i][hg][k + 2] - base);
+                        sum += S[i][hg][k] + S[i][hg][k + 2];
                     }
-                    l[hg] = l[hg] * f[hg] + sum;
+                    l[hg][k] = l[hg][k] * f[hg][k] + sum;
                 }
-                if (__any_sync(0xffffffffu, moved)) {
+            // P^T as the second operand: keys along the contraction
+            uint32_t ph[C::KT / 16][HG][2], pl[C::KT / 16][HG][2];
 #pragma unroll
-                    for (int n = 0; n < C::NT; ++n) {
-                        o[n][0] *= f[0];
-                        o[n][1] *= f[0];
-                        o[n][2] *= f[HG - 1];
-                        o[n][3] *= f[HG - 1];
-                    }
-                }
-                // O += P V
+            for (int i = 0; i < C::KT / 16; ++i)
 #pragma unroll
-                for (int v = 0; v < C::KT / 16; ++v)
+                for (int hg = 0; hg < HG; ++hg)
 #pragma unroll
-                    for (int c = 0; c < C::VC; ++c)
-#pragma unroll
-                        for (int e = 0; e < C::VE; ++e) {
-                            uint32_t b0, b1;
-                            if (E4M3) {
-                                const uint32_t sel = 0x40u + 0x11u * (e % 4);
-                                b0 = widen2(__byte_perm(V[v * 4][c][e / 4], V[v * 4 + 1][c][e / 4], sel));
-                                b1 = widen2(__byte_perm(V[v * 4 + 2][c][e / 4], V[v * 4 + 3][c][e / 4], sel));
-                            } else {
-                                const uint32_t sel = e % 2 ? 0x7632u : 0x5410u;
-                                b0 = __byte_perm(V[v * 4][c][e / 2], V[v * 4 + 1][c][e / 2], sel);
-                                b1 = __byte_perm(V[v * 4 + 2][c][e / 2], V[v * 4 + 3][c][e / 2], sel);
-                            }
-                            float (&acc)[4] = o[c * C::VE + e];
-                            if (HG == 1) {
-                                mma<C::F16>(acc, ph[2 * v][0], pl[2 * v][0], ph[2 * v + 1][0], pl[2 * v + 1][0], b0, b1);
-                            } else {
-                                mma<C::F16>(acc, ph[2 * v][0], ph[2 * v][HG - 1], ph[2 * v + 1][0], ph[2 * v + 1][HG - 1], b0, b1);
-                                if (!C::F16) mma<C::F16>(acc, pl[2 * v][0], pl[2 * v][HG - 1], pl[2 * v + 1][0], pl[2 * v + 1][HG - 1], b0, b1);
-                            }
+                    for (int h = 0; h < 2; ++h) {
+                        const float x = S[i][hg][2 * h], y = S[i][hg][2 * h + 1];
+                        const uint32_t p = pack2<C::F16>(x, y);
+                        ph[i][hg][h] = transpose8(p);
+                        if (!C::F16) {
+                            const float2 back = unpack2<C::F16>(p);
+                            pl[i][hg][h] = transpose8(pack2<C::F16>(x - back.x, y - back.y));
                         }
-                if (s + 1 < hi) load_V(off_next);
-                off = off_next;
-            }
-
-            // ---- the four warps' results, joined through shared memory
+                    }
+            if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
-            for (int hg = 0; hg < HG; ++hg) {
-                l[hg] += __shfl_xor_sync(0xffffffffu, l[hg], 1);
-                l[hg] += __shfl_xor_sync(0xffffffffu, l[hg], 2);
-                if (t == 0) {
-                    sM[warp * C::ROWS + hg * 8 + g] = m[hg];
-                    sL[warp * C::ROWS + hg * 8 + g] = l[hg];
+                for (int n = 0; n < C::NT; ++n)
+#pragma unroll
+                    for (int hg = 0; hg < HG; ++hg)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) o[n][hg][k] *= f[hg][k & 1];
+            }
+            // O^T += V^T P^T
+#pragma unroll
+            for (int i = 0; i < C::KT / 16; ++i)
+#pragma unroll
+                for (int c = 0; c < C::VC; ++c)
+#pragma unroll
+                    for (int e = 0; e < C::VE; e += 2) {
+                        uint32_t a0, a1, a2, a3;
+                        if (E4M3) {
+                            const uint32_t sel = e % 4 ? 0x7362u : 0x5140u;
+                            widen4(__byte_perm(V[i * 4][c][e / 4], V[i * 4 + 1][c][e / 4], sel), a0, a1);
+                            widen4(__byte_perm(V[i * 4 + 2][c][e / 4], V[i * 4 + 3][c][e / 4], sel), a2, a3);
+                        } else {
+                            a0 = __byte_perm(V[i * 4][c][e / 2], V[i * 4 + 1][c][e / 2], 0x5410u);
+                            a1 = __byte_perm(V[i * 4][c][e / 2], V[i * 4 + 1][c][e / 2], 0x7632u);
+                            a2 = __byte_perm(V[i * 4 + 2][c][e / 2], V[i * 4 + 3][c][e / 2], 0x5410u);
+                            a3 = __byte_perm(V[i * 4 + 2][c][e / 2], V[i * 4 + 3][c][e / 2], 0x7632u);
+                        }
+#pragma unroll
+                        for (int hg = 0; hg < HG; ++hg) {
+                            float (&acc)[4] = o[(c * C::VE + e) / 2][hg];
+                            mma<C::F16>(acc, a0, a1, a2, a3, ph[i][hg][0], ph[i][hg][1]);
+                            if (!C::F16) mma<C::F16>(acc, a0, a1, a2, a3, pl[i][hg][0], pl[i][hg][1]);
+                        }
+                    }
+            if (more) load_V(off_next, valid_next == kFull);
+            valid = valid_next;
+        }
+
+        // ---- the four warps' results, joined through shared memory
+#pragma unroll
+        for (int hg = 0; hg < HG; ++hg)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                float sum = l[hg][k];
+                sum += __shfl_xor_sync(0xffffffffu, sum, 4);
+                sum += __shfl_xor_sync(0xffffffffu, sum, 8);
+                sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+                const int row = hg * 8 + 2 * t + k;
+                if (g == 0) {
+                    sM[warp * C::ROWS + row] = m[hg][k];
+                    sL[warp * C::ROWS + row] = sum;
                 }
-                if (hg * 8 + g < rows) {
-                    float* row = sO + (warp * C::ROWS + hg * 8 + g) * C::LD;
+                if (row < rows) {
+                    float* to = sO + (warp * C::ROWS + row) * C::LD + g * C::VE;
 #pragma unroll
                     for (int c = 0; c < C::VC; ++c)
 #pragma unroll
-                        for (int half = 0; half < 2; ++half)
-#pragma unroll
-                            for (int e = 0; e < C::VE; e += 4) {
-                                float4 x;
-                                float* xs = &x.x;
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) {
-                                    const float (&acc)[4] = o[c * C::VE + e + i];
-                                    xs[i] = HG == 1 ? acc[half] + acc[2 + half] : acc[hg * 2 + half];
-                                }
-                                *reinterpret_cast<float4*>(row + c * 8 * C::VE + (2 * t + half) * C::VE + e) = x;
-                            }
+                        for (int e = 0; e < C::VE; e += 4) {
+                            const int n = (c * C::VE + e) / 2;
+                            *reinterpret_cast<float4*>(to + c * 8 * C::VE + e) =
+                                make_float4(o[n][hg][k], o[n][hg][k + 2], o[n + 1][hg][k], o[n + 1][hg][k + 2]);
+                        }
                 }
             }
-            __syncthreads();
+        __syncthreads();
 
-            const int64_t first = at / share, last = (at + steps - 1) / share;      // CTAs that have a piece of the item
-            float* my_part = a.part + (size_t)(2 * blockIdx.x + (lo == 0)) * kPagedRows * (D + 2);
-            constexpr int PER = 4;                             // neighbouring columns a thread
-            const float v_scale = E4M3 && a.v_scale != nullptr ? a.v_scale[kv] : 1.f;
-            auto store = [&](int row, int d, const float (&x)[PER], float top, float sum) {
-                const float inv = sum == 0.f ? 0.f : v_scale / sum;
-                uint2 w;
-                w.x = pack2<F16Q>(x[0] * inv, x[1] * inv);
-                w.y = pack2<F16Q>(x[2] * inv, x[3] * inv);
-                *reinterpret_cast<uint2*>(a.O + (((int64_t)r * a.n_heads + head0 + row) * D + d) * 2) = w;
-                if (a.LSE != nullptr && d == 0) a.LSE[(int64_t)(head0 + row) * a.n_requests + r] = top * 0.6931471805599453f + logf(sum);
-            };
-            for (int i = tid; i < rows * (D / PER); i += kPaThreads) {
-                const int row = i / (D / PER), d = i % (D / PER) * PER;
-                float top = -INFINITY;
+        constexpr int PER = 4;                             // neighbouring columns a thread
+        constexpr size_t kPart = kPartWords<D>;
+        const bool whole = lo == 0 && hi == steps;
+        const float v_scale = E4M3 && a.v_scale != nullptr ? a.v_scale[kv] : 1.f;
+        const Rows<D, F16Q> out{a.O + ((int64_t)r * a.n_heads + head0) * D * 2,
+                                a.LSE == nullptr ? nullptr : a.LSE + (int64_t)head0 * a.n_requests + r, a.n_requests, v_scale};
+        float* my_part = a.part + (2 * blockIdx.x + (lo == 0)) * kPart;
+        for (int i = tid; i < rows * (D / PER); i += kPaThreads) {
+            const int row = i / (D / PER), d = i % (D / PER) * PER;
+            float top = -INFINITY;
 #pragma unroll
-                for (int w = 0; w < kPaWarps; ++w) top = fmaxf(top, sM[w * C::ROWS + row]);
-                const float base = top == -INFINITY ? 0.f : top;
-                float x[PER] = {0.f, 0.f, 0.f, 0.f}, sum = 0.f;
+            for (int w = 0; w < kPaWarps; ++w) top = fmaxf(top, sM[w * C::ROWS + row]);
+            const float base = top == -INFINITY ? 0.f : top;
+            float x[PER] = {0.f, 0.f, 0.f, 0.f}, sum = 0.f;
 #pragma unroll
-                for (int w = 0; w < kPaWarps; ++w) {
-                    const float f = ex2(sM[w * C::ROWS + row] - base);
-                    const float4 y = *reinterpret_cast<const float4*>(sO + (w * C::ROWS + row) * C::LD + d);
-                    sum += f * sL[w * C::ROWS + row];
-                    x[0] += f * y.x, x[1] += f * y.y, x[2] += f * y.z, x[3] += f * y.w;
-                }
-                if (whole) {
-                    store(row, d, x, top, sum);
-                } else {
-                    *reinterpret_cast<float4*>(my_part + row * D + d) = make_float4(x[0], x[1], x[2], x[3]);
-                    if (d == 0) {
-                        my_part[kPagedRows * D + row] = top;
-                        my_part[kPagedRows * D + kPagedRows + row] = sum;
-                    }
-                }
+            for (int w = 0; w < kPaWarps; ++w) {
+                const float fw = ex2(sM[w * C::ROWS + row] - base);
+                const float4 y = *reinterpret_cast<const float4*>(sO + (w * C::ROWS + row) * C::LD + d);
+                sum += fw * sL[w * C::ROWS + row];
+                x[0] += fw * y.x, x[1] += fw * y.y, x[2] += fw * y.z, x[3] += fw * y.w;
             }
-            if (!whole) {
-                // the pieces' CTAs count themselves in; the last one joins them, first piece first
+            if (whole) out.store(row, d, x, top, sum);
+            else put_part<D>(my_part, row, d, x, top, sum);
+        }
+        if (!whole) {
+            // cuts inside the item: those that did not move to its ends
+            const int64_t cut0 = (at + snap + share - 1) / share, cut1 = (at + cost - snap - 1) / share;
+            const int first = (int)cut0 - 1, n = (int)(cut1 - cut0) + 2, mine = (int)blockIdx.x - first;
+            // counts this CTA in; true for the last of n
+            auto arrive = [&](int32_t* ticket, int of) {
                 __threadfence();
                 __syncthreads();
-                if (tid == 0) last_flag = atomicAdd(a.tickets + first, 1) == (int)(last - first);
+                if (tid == 0) {
+                    last_flag = atomicAdd(ticket, 1) == of - 1;
+                    if (last_flag) *ticket = 0;
+                }
                 __syncthreads();
-                if (last_flag) {
-                    __threadfence();
-                    if (tid == 0) a.tickets[first] = 0;
-                    const int n = (int)(last - first) + 1;
-                    auto piece = [&](int p) { return a.part + (size_t)(2 * (first + p) + (p == 0)) * kPagedRows * (D + 2); };
-                    for (int i = tid; i < rows * (D / PER); i += kPaThreads) {
-                        const int row = i / (D / PER), d = i % (D / PER) * PER;
-                        float top = -INFINITY;
-                        for (int p = 0; p < n; ++p) top = fmaxf(top, __ldcg(piece(p) + kPagedRows * D + row));
-                        const float base = top == -INFINITY ? 0.f : top;
-                        float x[PER] = {0.f, 0.f, 0.f, 0.f}, sum = 0.f;
-#pragma unroll 4
-                        for (int p = 0; p < n; ++p) {
-                            const float* q = piece(p);
-                            const float f = ex2(__ldcg(q + kPagedRows * D + row) - base);
-                            const float4 y = __ldcg(reinterpret_cast<const float4*>(q + row * D + d));
-                            sum += f * __ldcg(q + kPagedRows * D + kPagedRows + row);
-                            x[0] += f * y.x, x[1] += f * y.y, x[2] += f * y.z, x[3] += f * y.w;
-                        }
-                        store(row, d, x, top, sum);
+                const bool last = last_flag;
+                if (last) __threadfence();
+                return last;
+            };
+            // counters: of the item; of its first group; of a later group, by the group's first CTA (which may also begin an item)
+            int32_t* tickets = a.tickets + first;
+            if (n <= kPaJoin) {
+                if (arrive(tickets, n)) join_pieces<D, F16Q>(a.part, first, 0, 1, n, rows, sO, &out);
+            } else {
+                // levels: groups of kPaJoin pieces, then their results
+                const int group = mine / kPaJoin, groups = (n + kPaJoin - 1) / kPaJoin, p0 = group * kPaJoin;
+                const int count = min(kPaJoin, n - p0);
+                if (arrive(tickets + kPaTicketRow * (group == 0 ? 1 : 2) + p0, count)) {
+                    join_pieces<D, F16Q>(a.part, first, p0, 1, count, rows, sO, nullptr);
+                    if (arrive(tickets, groups)) {
+                        // beyond kPaJoin^2 pieces one more level, by this CTA alone
+                        for (int q0 = 0; groups > kPaJoin && q0 < groups; q0 += kPaJoin)
+                            join_pieces<D, F16Q>(a.part, first, q0 * kPaJoin, kPaJoin, min(kPaJoin, groups - q0), rows, sO, nullptr);
+                        const int by = groups > kPaJoin ? kPaJoin * kPaJoin : kPaJoin;
+                        join_pieces<D, F16Q>(a.part, first, 0, by, (n + by - 1) / by, rows, sO, &out);
                     }
                 }
             }
-            __syncthreads();                    // shared memory is free for the next item
         }
-        at += steps + kPaItemCost;
+        at += cost;
         if (at >= end) break;
         if (++item == H) {
             item = 0;
             if (++r == a.n_requests) break;
-            kept = kept_of(a, ld_index(a.lens + r));
-            steps = max((kept.n + C::STEP - 1) / C::STEP, 1);
+            kept = kept_at(r);
         }
+        __syncthreads();                    // shared memory is free for the next item
     }
 }
 

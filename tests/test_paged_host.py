@@ -83,7 +83,7 @@ def test_a_missing_cache_is_refused(L):
 def test_workspace_is_checked(L):
     c = cache()
     need = L.pafu_paged_workspace_bytes(ctypes.byref(c))
-    assert need > 4608 and need % 256 == 0
+    assert need > 12800 and need % 256 == 0
     for call in (tables, append, attn):
         assert call(L, c, ws=None) == INVALID
         assert call(L, c, ws=FAKE + 40 * GB + 64) == MISALIGNED

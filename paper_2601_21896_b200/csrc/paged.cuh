@@ -1,6 +1,7 @@
 // What the kernels of the paged cache share: its geometry as the kernels see it, and the workspace's layout.
 #pragma once
 #include "common.cuh"
+#include "paged_plan.cuh"
 
 namespace pafu {
 
@@ -13,22 +14,6 @@ constexpr int kPagedCtasPerSm = 4;             // most CTAs of the attention ker
 constexpr int kPagedRows = 16;                 // query heads that one item handles (rows of a tensor-core tile)
 static_assert(kPagedCtasPerSm * kMaxPersistentGrid <= kPaTicketRow, "a ticket for every CTA");
 static_assert(kPagedPartOffset % 256 == 0 && kPagedPartOffset == PAFU_PAGED_HEADER_BYTES, "the part of the workspace that starts at zero");
-
-// n / d for 0 <= n < 2^31 as a product: m = floor(2^(31+s) / d) + 1 with s = ceil(log2 d) has an excess below
-// 2^(31+s) / 2^31, so the quotient is exact (round-up method of division by an invariant integer).
-struct FastDiv {
-    uint32_t d, m, s;
-};
-inline FastDiv fast_div(uint32_t d) {
-    uint32_t s = 0;
-    while ((1ull << s) < d) ++s;
-    return FastDiv{d, (uint32_t)(((1ull << (31 + s)) / d) + 1), s};
-}
-#ifdef __CUDACC__
-__device__ __forceinline__ uint32_t div_by(uint32_t n, const FastDiv& f) {
-    return (uint32_t)(((uint64_t)n * f.m) >> (31 + f.s));
-}
-#endif
 
 // The pools, with strides in 16-byte units.
 struct PagedPool {

@@ -19,7 +19,7 @@
 // Split over the length: every (request, group of heads) is an item of ceil(kept / step) steps (a step is one tile for each of
 // the four warps) and a fixed cost.  All items laid end to end are cut into equal shares, one a CTA, by arithmetic that every
 // CTA does for itself from the lengths on the device: the grid does not depend on the lengths, and a captured launch follows
-// them.  A cut that would leave less than a few steps of an item on one side moves to the item's end.  A share's first and last
+// them.  A cut that would leave few steps of an item on one side moves to the item's end.  A share's first and last
 // item may continue in other CTAs: their fp32 partial results go to the workspace, and the CTA that arrives last
 // (a counter; nothing waits) joins them in a fixed order, so results do not depend on timing; more than 16 pieces are joined
 // in groups of 16 first, by as many CTAs.
@@ -35,9 +35,6 @@ namespace {
 
 constexpr int kPaWarps = 4;
 constexpr int kPaThreads = kPaWarps * 32;
-constexpr int kPaItemCost = 1;        // what an item costs beside its steps, in steps
-constexpr int kPaMinShare = 4;        // steps and item costs that a CTA takes at least
-constexpr int kPaSnap = 4;            // a cut this near to an item's end moves there
 constexpr int kPaJoin = 16;           // pieces that are joined at once
 static_assert(3 * kPaTicketRow < kPagedTickets, "three counters a CTA, and the tables' own");
 
@@ -186,8 +183,13 @@ __device__ __forceinline__ uint32_t key_offset(const PagedAttnArgs& a, const Key
 
 // Where a CTA begins or ends: a position on the line of all items, and the request and item it lies in.
 struct Cut {
-    int64_t at, item_at;      // the position; where its item begins
+    uint64_t at, item_at;     // the position; where its item begins
     int32_t r, item;
+};
+// A CTA's part of an item: steps [lo, hi) of `steps`; pos: where the item begins, seen from the CTA's first position.
+struct Work {
+    int32_t r, item, pos, steps, lo, hi;
+    Kept kept;
 };
 
 // Where an item's heads go, and how
@@ -262,7 +264,7 @@ __global__ void __launch_bounds__(kPaThreads, (Tile<D, F16Q, E4M3, HG>::CTAS)) p
     float* sO = sm;                                   // [warp][row][LD]
     float* sM = sm + kPaWarps * C::ROWS * C::LD;      // [warp][row]
     float* sL = sM + kPaWarps * C::ROWS;
-    __shared__ int64_t plan_sum[kPaWarps];
+    __shared__ uint64_t plan_sum[kPaWarps];
     __shared__ Cut cuts[2];
     __shared__ int32_t last_flag;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
@@ -273,50 +275,57 @@ __global__ void __launch_bounds__(kPaThreads, (Tile<D, F16Q, E4M3, HG>::CTAS)) p
     // ---- this CTA's share of all steps
     auto kept_at = [&](int r) { return kept_of(a, ld_index(a.lens + r)); };
     auto steps_of = [](const Kept& k) { return max((k.n + C::STEP - 1) / C::STEP, 1); };
-    int64_t share;
-    int snap;
+    PagedCuts plan;
     {
         const int per = (a.n_requests + kPaThreads - 1) / kPaThreads;
         const int r0 = min(tid * per, a.n_requests), r1 = min(r0 + per, a.n_requests);
-        int64_t mine = 0;
-        for (int r = r0; r < r1; ++r) mine += steps_of(kept_at(r)) + kPaItemCost;
-        int64_t inc = mine;
+        uint64_t mine = 0;
+        for (int r = r0; r < r1; r += 4) {
+            int32_t T[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) T[i] = r + i < r1 ? ld_index(a.lens + r + i) : 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (r + i < r1) mine += steps_of(kept_of(a, T[i])) + kPaItemCost;
+        }
+        uint64_t inc = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const int64_t v = __shfl_up_sync(0xffffffffu, inc, o);
+            const uint64_t v = __shfl_up_sync(0xffffffffu, inc, o);
             if (lane >= o) inc += v;
         }
         if (lane == 31) plan_sum[warp] = inc;
         __syncthreads();
-        int64_t all = 0, before = inc - mine;
+        uint64_t all = 0, before = inc - mine;
+#pragma unroll
         for (int w = 0; w < kPaWarps; ++w) {
             if (w < warp) before += plan_sum[w];
             all += plan_sum[w];
         }
-        all *= H;
         before *= H;
-        share = max((all + gridDim.x - 1) / gridDim.x, (int64_t)kPaMinShare);
-        snap = (int)min(share / 2, (int64_t)kPaSnap);
-        if (share * blockIdx.x >= all) return;
+        plan = paged_cuts(all * H, gridDim.x);
+        if (blockIdx.x >= plan.n) return;
+        const uint64_t b0 = paged_cut(plan, blockIdx.x), b1 = paged_cut(plan, blockIdx.x + 1);
+#pragma unroll 1
         for (int i = 0; i < 2; ++i) {
-            const int64_t b = share * (blockIdx.x + i);
-            if (b >= all) {
-                if (tid == 0) cuts[i] = Cut{all, all, a.n_requests, 0};
+            const uint64_t b = i ? b1 : b0;
+            if (b >= plan.all) {
+                if (tid == 0) cuts[i] = Cut{plan.all, plan.all, a.n_requests, 0};
             } else if (b >= before && b < before + mine * H) {
-                int64_t at = before;
+                uint64_t at = before;
                 int r = r0, cost = 0;
                 for (; r < r1; ++r) {
                     cost = steps_of(kept_at(r)) + kPaItemCost;
-                    if (b < at + (int64_t)H * cost) break;
-                    at += (int64_t)H * cost;
+                    if (b < at + (uint64_t)H * cost) break;
+                    at += (uint64_t)H * cost;
                 }
                 Cut c;
                 c.r = r;
-                c.item = (int)((b - at) / cost);
-                c.item_at = at + (int64_t)c.item * cost;
-                const int o = (int)(b - c.item_at);
-                c.at = o < snap ? c.item_at : b;
-                if (o >= snap && cost - o <= snap) {             // on to the next item
+                c.item = (int)div_u64(b - at, cost);
+                c.item_at = at + (uint64_t)c.item * cost;
+                const int moves = paged_cut_moves(plan, (int)(b - c.item_at), cost);
+                c.at = moves < 0 ? c.item_at : b;
+                if (moves > 0) {                                 // on to the next item
                     c.item_at += cost;
                     c.at = c.item_at;
                     if (++c.item == H) c.item = 0, ++c.r;
@@ -326,83 +335,113 @@ __global__ void __launch_bounds__(kPaThreads, (Tile<D, F16Q, E4M3, HG>::CTAS)) p
         }
         __syncthreads();
     }
-    const int64_t begin = cuts[0].at, end = cuts[1].at;
-    if (begin >= end) return;
-    int r = cuts[0].r, item = cuts[0].item;
-    int64_t at = cuts[0].item_at;                     // where the item starts
-    Kept kept = kept_at(r);
+    const int length = (int)((int64_t)cuts[1].at - (int64_t)cuts[0].at);
+    if (length <= 0) return;
 
-    while (true) {
-        const int steps = steps_of(kept), cost = steps + kPaItemCost;
-        const int lo = (int)max(begin - at, (int64_t)0);
-        const int hi = (int)min((int64_t)steps, end - at);
-        const int kv = item / a.parts, head0 = kv * a.group + (item - kv * a.parts) * kPagedRows;
-        const int rows = min(kPagedRows, (kv + 1) * a.group - head0);       // query heads of the item
-        const int32_t* table = a.pool.table + (int64_t)r * a.pool.max_pages;
-        const uint32_t head_u = (uint32_t)kv * a.pool.head_u;
+    auto enter = [&](Work& w) {
+        w.steps = steps_of(w.kept);
+        w.lo = max(-w.pos, 0);
+        w.hi = min(w.steps, length - w.pos);
+    };
+    auto advance = [&](const Work& w, Work& x) {
+        x = w;
+        x.pos = w.pos + w.steps + kPaItemCost;
+        if (x.pos >= length) return false;
+        if (++x.item == H) {
+            x.item = 0;
+            if (++x.r == a.n_requests) return false;
+            x.kept = kept_at(x.r);
+        }
+        enter(x);
+        return true;
+    };
+    Work w;
+    w.r = cuts[0].r;
+    w.item = cuts[0].item;
+    w.pos = (int)((int64_t)cuts[0].item_at - (int64_t)cuts[0].at);
+    w.kept = kept_at(w.r);
+    enter(w);
 
-        uint32_t K[C::KR][C::KW / 4][4], V[C::VR][C::VC][C::VB / 4];
-        auto load_K = [&](uint32_t off, bool full) {
+    // ---- rows and queries on their way
+    uint32_t K[C::KR][C::KW / 4][4], V[C::VR][C::VC][C::VB / 4], qf[HG][D / 16][2];
+    auto load_K = [&](uint32_t off, bool full) {
 #pragma unroll
-            for (int i = 0; i < C::KR; ++i) {
-                const uint32_t o = __shfl_sync(0xffffffffu, off, i * 8 + g);
-                const char* p = a.pool.K + (uint64_t)o * 16 + t * 16;
+        for (int i = 0; i < C::KR; ++i) {
+            const uint32_t o = __shfl_sync(0xffffffffu, off, i * 8 + g);
+            const char* p = a.pool.K + (uint64_t)o * 16 + t * 16;
 #pragma unroll
-                for (int c = 0; c < C::KW / 4; ++c) {
-                    if (full) ld_row(K[i][c], p + c * 64);
-                    else ld_row(K[i][c], p + c * 64, o != ~0u);
-                }
+            for (int c = 0; c < C::KW / 4; ++c) {
+                if (full) ld_row(K[i][c], p + c * 64);
+                else ld_row(K[i][c], p + c * 64, o != ~0u);
             }
-        };
-        auto load_V = [&](uint32_t off, bool full) {
+        }
+    };
+    auto load_V = [&](uint32_t off, bool full) {
 #pragma unroll
-            for (int i = 0; i < C::VR; ++i) {
-                const uint32_t o = __shfl_sync(0xffffffffu, off, (i >> 2) * 16 + ((i >> 1) & 1) * 8 + 2 * t + (i & 1));
-                const char* p = a.pool.V + (uint64_t)o * 16 + g * C::VB;
+        for (int i = 0; i < C::VR; ++i) {
+            const uint32_t o = __shfl_sync(0xffffffffu, off, (i >> 2) * 16 + ((i >> 1) & 1) * 8 + 2 * t + (i & 1));
+            const char* p = a.pool.V + (uint64_t)o * 16 + g * C::VB;
 #pragma unroll
-                for (int c = 0; c < C::VC; ++c) {
-                    if (full) ld_row(V[i][c], p + c * 8 * C::VB);
-                    else ld_row(V[i][c], p + c * 8 * C::VB, o != ~0u);
-                }
+            for (int c = 0; c < C::VC; ++c) {
+                if (full) ld_row(V[i][c], p + c * 8 * C::VB);
+                else ld_row(V[i][c], p + c * 8 * C::VB, o != ~0u);
             }
-        };
-        auto valid_of = [](uint32_t off) {
-            return __ballot_sync(0xffffffffu, off != ~0u) & (C::KT == 32 ? ~0u : (1u << C::KT % 32) - 1u);
-        };
-        constexpr uint32_t kFull = C::KT == 32 ? ~0u : (1u << C::KT % 32) - 1u;
-
-        // the first tile's rows are requested before the queries
-        int32_t j = (lo * kPaWarps + warp) * C::KT + (lane & (C::KT - 1));
-        const int32_t j_end = hi * C::STEP;           // exclusive; keys past kept.n do not exist
-        auto ask = [&](int32_t jj) { return key_at(a, kept, table, jj < j_end ? jj : 0x7fffffff, head_u); };
-        uint32_t off = key_offset(a, ask(j));
-        KeyAt next = ask(j + C::STEP);
-        uint32_t valid = valid_of(off);
-        load_K(off, valid == kFull);
-        load_V(off, valid == kFull);
-
-        // queries: head g (and g + 8), in the order in which the lane's key words come
-        uint32_t qf[HG][D / 16][2];
-        float c_col[HG][2];                           // factor of the logits of heads 2t, 2t + 1
+        }
+    };
+    constexpr uint32_t kFull = C::KT == 32 ? ~0u : (1u << C::KT % 32) - 1u;
+    auto valid_of = [&](uint32_t off) { return __ballot_sync(0xffffffffu, off != ~0u) & kFull; };
+    // key `j` of the item's kept ones, if it is one of this CTA's
+    auto ask = [&](const Work& w, int32_t j) {
+        return key_at(a, w.kept, a.pool.table + (int64_t)w.r * a.pool.max_pages, j < w.hi * C::STEP ? j : 0x7fffffff,
+                      (uint32_t)(w.item / a.parts) * a.pool.head_u);
+    };
+    auto first_key = [&](const Work& w) { return (w.lo * kPaWarps + warp) * C::KT + (lane & (C::KT - 1)); };
+    // the item's first query head, and how many heads it has
+    auto head0_of = [&](const Work& w) { const int kv = w.item / a.parts; return kv * a.group + (w.item - kv * a.parts) * kPagedRows; };
+    auto rows_of = [&](const Work& w) { return min(kPagedRows, (w.item / a.parts + 1) * a.group - head0_of(w)); };
+    // queries: head g (and g + 8), in the order in which the lane's key words come
+    auto load_Q = [&](const Work& w) {
+        const int head0 = head0_of(w), rows = rows_of(w);
 #pragma unroll
         for (int hg = 0; hg < HG; ++hg) {
             const bool have = hg * 8 + g < rows;
-            const char* qp = a.Q + r * a.q_token + (int64_t)(head0 + hg * 8 + g) * a.q_head;
+            const char* qp = a.Q + w.r * a.q_token + (int64_t)(head0 + hg * 8 + g) * a.q_head;
 #pragma unroll
             for (int c = 0; c < C::KW / 4; ++c) {
                 constexpr int PER = 16 / C::ES;       // elements of 16 bytes of a key row
                 const char* p = qp + (c * 4 * PER + t * PER) * 2;
 #pragma unroll
                 for (int h = 0; h < PER / 8; ++h) {
-                    uint4 w = make_uint4(0, 0, 0, 0);
-                    if (have) w = *reinterpret_cast<const uint4*>(p + h * 16);
+                    uint32_t q[4];
+                    ld_row(q, p + h * 16, have);
                     const int ks = c * (PER / 4) + h * 2;
-                    qf[hg][ks][0] = w.x;
-                    qf[hg][ks][1] = w.y;
-                    qf[hg][ks + 1][0] = w.z;
-                    qf[hg][ks + 1][1] = w.w;
+                    qf[hg][ks][0] = q[0];
+                    qf[hg][ks][1] = q[1];
+                    qf[hg][ks + 1][0] = q[2];
+                    qf[hg][ks + 1][1] = q[3];
                 }
             }
+        }
+    };
+
+    int32_t j = first_key(w);
+    uint32_t off = key_offset(a, ask(w, j));
+    KeyAt next = ask(w, j + C::STEP);
+    uint32_t valid = valid_of(off);
+    load_K(off, valid == kFull);
+    load_V(off, valid == kFull);
+    load_Q(w);
+
+    while (true) {
+        // the next item's first rows are looked up now and requested behind this item's last ones
+        Work x;
+        const bool another = advance(w, x);
+        const KeyAt x_key = another ? ask(x, first_key(x)) : KeyAt{0, ~0u};
+
+        float c_col[HG][2];                           // factor of the logits of heads 2t, 2t + 1
+        const int kv = w.item / a.parts;
+#pragma unroll
+        for (int hg = 0; hg < HG; ++hg) {
             float c_row = a.scale;
             if (E4M3 && a.k_scale != nullptr) c_row *= a.k_scale[kv];
             if (E4M3 && !F16Q) {
@@ -442,12 +481,12 @@ __global__ void __launch_bounds__(kPaThreads, (Tile<D, F16Q, E4M3, HG>::CTAS)) p
 #pragma unroll
         for (int hg = 0; hg < HG; ++hg) m[hg][0] = m[hg][1] = -INFINITY, l[hg][0] = l[hg][1] = 0.f;
 
-        for (int s = lo; s < hi; ++s) {
+        for (int s = w.lo; s < w.hi; ++s) {
             const uint32_t off_next = key_offset(a, next);
             j += C::STEP;
-            next = ask(j + C::STEP);
+            next = ask(w, j + C::STEP);
             const uint32_t valid_next = valid_of(off_next);
-            const bool more = s + 1 < hi;
+            const bool more = s + 1 < w.hi;
             if (valid == 0u) {                        // a short item: nothing for this warp
                 if (more) {
                     load_K(off_next, false);
@@ -575,6 +614,19 @@ __global__ void __launch_bounds__(kPaThreads, (Tile<D, F16Q, E4M3, HG>::CTAS)) p
             valid = valid_next;
         }
 
+        auto request = [&] {
+            off = key_offset(a, x_key);
+            valid = valid_of(off);
+            load_K(off, valid == kFull);
+            load_V(off, valid == kFull);
+            load_Q(x);
+            j = first_key(x);
+            next = ask(x, j + C::STEP);
+        };
+        const bool whole = w.lo == 0 && w.hi == w.steps;
+        if (another && whole) request();              // (not across the call that joins pieces)
+
+        const int head0 = head0_of(w), rows = rows_of(w);
         // ---- the four warps' results, joined through shared memory
 #pragma unroll
         for (int hg = 0; hg < HG; ++hg)
@@ -605,32 +657,30 @@ __global__ void __launch_bounds__(kPaThreads, (Tile<D, F16Q, E4M3, HG>::CTAS)) p
 
         constexpr int PER = 4;                             // neighbouring columns a thread
         constexpr size_t kPart = kPartWords<D>;
-        const bool whole = lo == 0 && hi == steps;
         const float v_scale = E4M3 && a.v_scale != nullptr ? a.v_scale[kv] : 1.f;
-        const Rows<D, F16Q> out{a.O + ((int64_t)r * a.n_heads + head0) * D * 2,
-                                a.LSE == nullptr ? nullptr : a.LSE + (int64_t)head0 * a.n_requests + r, a.n_requests, v_scale};
-        float* my_part = a.part + (2 * blockIdx.x + (lo == 0)) * kPart;
+        const Rows<D, F16Q> out{a.O + ((int64_t)w.r * a.n_heads + head0) * D * 2,
+                                a.LSE == nullptr ? nullptr : a.LSE + (int64_t)head0 * a.n_requests + w.r, a.n_requests, v_scale};
+        float* my_part = a.part + (2 * blockIdx.x + (w.lo == 0)) * kPart;
         for (int i = tid; i < rows * (D / PER); i += kPaThreads) {
             const int row = i / (D / PER), d = i % (D / PER) * PER;
             float top = -INFINITY;
 #pragma unroll
-            for (int w = 0; w < kPaWarps; ++w) top = fmaxf(top, sM[w * C::ROWS + row]);
+            for (int i4 = 0; i4 < kPaWarps; ++i4) top = fmaxf(top, sM[i4 * C::ROWS + row]);
             const float base = top == -INFINITY ? 0.f : top;
             float x[PER] = {0.f, 0.f, 0.f, 0.f}, sum = 0.f;
 #pragma unroll
-            for (int w = 0; w < kPaWarps; ++w) {
-                const float fw = ex2(sM[w * C::ROWS + row] - base);
-                const float4 y = *reinterpret_cast<const float4*>(sO + (w * C::ROWS + row) * C::LD + d);
-                sum += fw * sL[w * C::ROWS + row];
+            for (int i4 = 0; i4 < kPaWarps; ++i4) {
+                const float fw = ex2(sM[i4 * C::ROWS + row] - base);
+                const float4 y = *reinterpret_cast<const float4*>(sO + (i4 * C::ROWS + row) * C::LD + d);
+                sum += fw * sL[i4 * C::ROWS + row];
                 x[0] += fw * y.x, x[1] += fw * y.y, x[2] += fw * y.z, x[3] += fw * y.w;
             }
             if (whole) out.store(row, d, x, top, sum);
             else put_part<D>(my_part, row, d, x, top, sum);
         }
         if (!whole) {
-            // cuts inside the item: those that did not move to its ends
-            const int64_t cut0 = (at + snap + share - 1) / share, cut1 = (at + cost - snap - 1) / share;
-            const int first = (int)cut0 - 1, n = (int)(cut1 - cut0) + 2, mine = (int)blockIdx.x - first;
+            const PagedPieces p = paged_pieces(plan, cuts[0].at + (int64_t)w.pos, w.steps + kPaItemCost);
+            const int first = p.first, n = p.n, mine = (int)blockIdx.x - first;
             // counts this CTA in; true for the last of n
             auto arrive = [&](int32_t* ticket, int of) {
                 __threadfence();
@@ -664,13 +714,9 @@ __global__ void __launch_bounds__(kPaThreads, (Tile<D, F16Q, E4M3, HG>::CTAS)) p
                 }
             }
         }
-        at += cost;
-        if (at >= end) break;
-        if (++item == H) {
-            item = 0;
-            if (++r == a.n_requests) break;
-            kept = kept_at(r);
-        }
+        if (!another) break;
+        if (!whole) request();
+        w = x;
         __syncthreads();                    // shared memory is free for the next item
     }
 }

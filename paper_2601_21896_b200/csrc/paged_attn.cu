@@ -61,22 +61,21 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 
-// 16 (8) bytes of a row
-__device__ __forceinline__ void ld_row(uint32_t (&w)[4], const char* p) {
-    asm volatile("ld.global.nc.L1::no_allocate.L2::128B.v4.u32 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p) : "memory");
-}
-__device__ __forceinline__ void ld_row(uint32_t (&w)[2], const char* p) {
-    asm volatile("ld.global.nc.L1::no_allocate.L2::128B.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p) : "memory");
-}
-// the same, or zeros
+// 16 (8) bytes of a row, or zeros.  (Predicated in one piece: as a branch, or with a second copy of the loads for whole tiles, the loop
+// over the keys runs 4 to 8 % longer.)
 __device__ __forceinline__ void ld_row(uint32_t (&w)[4], const char* p, bool ok) {
     w[0] = w[1] = w[2] = w[3] = 0u;
-    if (ok) ld_row(w, p);
+    asm volatile(
+        "{\n\t.reg .pred P;\n\tsetp.ne.b32 P, %5, 0;\n\t"
+        "@P ld.global.nc.L1::no_allocate.L2::128B.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
+        : "+r"(w[0]), "+r"(w[1]), "+r"(w[2]), "+r"(w[3]) : "l"(p), "r"((int)ok) : "memory");
 }
 __device__ __forceinline__ void ld_row(uint32_t (&w)[2], const char* p, bool ok) {
     w[0] = w[1] = 0u;
-    if (ok) ld_row(w, p);
+    asm volatile(
+        "{\n\t.reg .pred P;\n\tsetp.ne.b32 P, %3, 0;\n\t"
+        "@P ld.global.nc.L1::no_allocate.L2::128B.v2.u32 {%0, %1}, [%2];\n\t}"
+        : "+r"(w[0]), "+r"(w[1]) : "l"(p), "r"((int)ok) : "memory");
 }
 
 template <bool F16>
@@ -154,7 +153,6 @@ struct Tile {
     static constexpr int CTAS = HG * D <= 128 ? 3 : 2;            // an SM: 168 or 255 registers a thread
     static constexpr size_t SMEM = sizeof(float) * (kPaWarps * ROWS * LD + 2 * kPaWarps * ROWS);
     static_assert(KT % 16 == 0 && VE % 4 == 0, "fragments");
-    static_assert(2 * kPaJoin * kPagedRows <= kPaWarps * ROWS * LD, "the pieces' maxima and sums fit where the warps' results were");
 };
 
 // Address of a key: its row of the pools in 16-byte units (head included), or ~0
@@ -199,21 +197,25 @@ struct Rows {
     float* LSE;
     int32_t lse_stride;
     float v_scale;
-    __device__ void store(int row, int d, const float (&x)[4], float top, float sum) const {
+    template <int PER>
+    __device__ __forceinline__ void store(int row, int d, const float (&x)[PER], float top, float sum) const {
         const float inv = sum == 0.f ? 0.f : v_scale / sum;
-        uint2 w;
-        w.x = pack2<F16Q>(x[0] * inv, x[1] * inv);
-        w.y = pack2<F16Q>(x[2] * inv, x[3] * inv);
-        *reinterpret_cast<uint2*>(O + ((int64_t)row * D + d) * 2) = w;
+        uint32_t w[PER / 2];
+#pragma unroll
+        for (int i = 0; i < PER / 2; ++i) w[i] = pack2<F16Q>(x[2 * i] * inv, x[2 * i + 1] * inv);
+        char* to = O + ((int64_t)row * D + d) * 2;
+        if (PER == 4) *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[PER / 2 - 1]);
+        else *reinterpret_cast<uint32_t*>(to) = w[0];
         if (LSE != nullptr && d == 0) LSE[(int64_t)row * lse_stride] = top * 0.6931471805599453f + logf(sum);
     }
 };
 // A piece's results in the workspace: numerators, maxima, sums
 template <int D>
 constexpr size_t kPartWords = (size_t)kPagedRows * (D + 2);
-template <int D>
-__device__ __forceinline__ void put_part(float* part, int row, int d, const float (&x)[4], float top, float sum) {
-    *reinterpret_cast<float4*>(part + row * D + d) = make_float4(x[0], x[1], x[2], x[3]);
+template <int D, int PER>
+__device__ __forceinline__ void put_part(float* part, int row, int d, const float (&x)[PER], float top, float sum) {
+    if (PER == 4) *reinterpret_cast<float4*>(part + row * D + d) = make_float4(x[0], x[1], x[PER - 2], x[PER - 1]);
+    else *reinterpret_cast<float2*>(part + row * D + d) = make_float2(x[0], x[1]);
     if (d == 0) {
         part[kPagedRows * D + row] = top;
         part[kPagedRows * D + kPagedRows + row] = sum;
@@ -221,40 +223,49 @@ __device__ __forceinline__ void put_part(float* part, int row, int d, const floa
 }
 
 // Pieces p0, p0 + by, ... (count <= kPaJoin) of the item whose first piece is CTA `first`'s, joined by the whole CTA: to the output, or in
-// place of piece p0.  A call, so that its registers do not count in the loop over the keys.
+// place of piece p0.  One trip to L2 for a warp's rows: everything is requested before anything is used.  A call, so that its registers do not
+// count in the loop over the keys.
 template <int D, bool F16Q>
-__device__ __noinline__ void join_pieces(float* parts, int first, int p0, int by, int count, int rows, float* shared, const Rows<D, F16Q>* out) {
-    constexpr int PER = 4, COLS = D / PER;
-    const int tid = threadIdx.x;
-    float* jm = shared;                                      // [piece][row]
-    float* jl = shared + kPaJoin * kPagedRows;
+__device__ __noinline__ void join_pieces(float* parts, int first, int p0, int by, int count, int rows, const Rows<D, F16Q>* out) {
+    constexpr int PER = D / 32;                              // columns a lane: a warp has a row
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, d = lane * PER;
     auto piece = [&](int i) { const int p = p0 + i * by; return parts + (2 * (size_t)(first + p) + (p == 0)) * kPartWords<D>; };
-    __syncthreads();
-    for (int i = tid; i < count * kPagedRows; i += kPaThreads) {
-        const float* q = piece(i / kPagedRows) + kPagedRows * D + i % kPagedRows;
-        if (i % kPagedRows < rows) jm[i] = __ldcg(q), jl[i] = __ldcg(q + kPagedRows);
-    }
-    __syncthreads();
-    for (int i = tid; i < rows * COLS; i += kPaThreads) {
-        const int row = i / COLS, d = i % COLS * PER;
-        float4 y[kPaJoin];
+    for (int row = warp; row < rows; row += kPaWarps) {
+        float y[kPaJoin][PER], m[kPaJoin], l[kPaJoin];
 #pragma unroll
-        for (int p = 0; p < kPaJoin; ++p) y[p] = p < count ? __ldcg(reinterpret_cast<const float4*>(piece(p) + row * D + d)) : make_float4(0.f, 0.f, 0.f, 0.f);
-        float top = -INFINITY;
-        for (int p = 0; p < count; ++p) top = fmaxf(top, jm[p * kPagedRows + row]);
-        const float base = top == -INFINITY ? 0.f : top;
-        float x[PER] = {0.f, 0.f, 0.f, 0.f}, sum = 0.f;
+        for (int p = 0; p < kPaJoin; ++p) {
+            m[p] = -INFINITY;
+            l[p] = 0.f;
 #pragma unroll
-        for (int p = 0; p < kPaJoin; ++p)
+            for (int k = 0; k < PER; ++k) y[p][k] = 0.f;
             if (p < count) {
-                const float f = ex2(jm[p * kPagedRows + row] - base);
-                sum += f * jl[p * kPagedRows + row];
-                x[0] += f * y[p].x, x[1] += f * y[p].y, x[2] += f * y[p].z, x[3] += f * y[p].w;
+                const float* q = piece(p);
+                m[p] = __ldcg(q + kPagedRows * D + row);
+                l[p] = __ldcg(q + kPagedRows * D + kPagedRows + row);
+                if (PER == 4) {
+                    const float4 v = __ldcg(reinterpret_cast<const float4*>(q + row * D + d));
+                    y[p][0] = v.x, y[p][1] = v.y, y[p][PER - 2] = v.z, y[p][PER - 1] = v.w;
+                } else {
+                    const float2 v = __ldcg(reinterpret_cast<const float2*>(q + row * D + d));
+                    y[p][0] = v.x, y[p][1] = v.y;
+                }
             }
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int p = 0; p < kPaJoin; ++p) top = fmaxf(top, m[p]);
+        const float base = top == -INFINITY ? 0.f : top;
+        float x[PER] = {}, sum = 0.f;
+#pragma unroll
+        for (int p = 0; p < kPaJoin; ++p) {
+            const float f = ex2(m[p] - base);
+            sum += f * l[p];
+#pragma unroll
+            for (int k = 0; k < PER; ++k) x[k] += f * y[p][k];
+        }
         if (out != nullptr) out->store(row, d, x, top, sum);
         else put_part<D>(piece(0), row, d, x, top, sum);
     }
-    __syncthreads();
 }
 
 template <int D, bool F16Q, bool E4M3, int HG>
@@ -364,27 +375,25 @@ __global__ void __launch_bounds__(kPaThreads, (Tile<D, F16Q, E4M3, HG>::CTAS)) p
 
     // ---- rows and queries on their way
     uint32_t K[C::KR][C::KW / 4][4], V[C::VR][C::VC][C::VB / 4], qf[HG][D / 16][2];
-    auto load_K = [&](uint32_t off, bool full) {
+    auto load_K = [&](uint32_t off) {
 #pragma unroll
         for (int i = 0; i < C::KR; ++i) {
             const uint32_t o = __shfl_sync(0xffffffffu, off, i * 8 + g);
             const char* p = a.pool.K + (uint64_t)o * 16 + t * 16;
 #pragma unroll
             for (int c = 0; c < C::KW / 4; ++c) {
-                if (full) ld_row(K[i][c], p + c * 64);
-                else ld_row(K[i][c], p + c * 64, o != ~0u);
+                ld_row(K[i][c], p + c * 64, o != ~0u);
             }
         }
     };
-    auto load_V = [&](uint32_t off, bool full) {
+    auto load_V = [&](uint32_t off) {
 #pragma unroll
         for (int i = 0; i < C::VR; ++i) {
             const uint32_t o = __shfl_sync(0xffffffffu, off, (i >> 2) * 16 + ((i >> 1) & 1) * 8 + 2 * t + (i & 1));
             const char* p = a.pool.V + (uint64_t)o * 16 + g * C::VB;
 #pragma unroll
             for (int c = 0; c < C::VC; ++c) {
-                if (full) ld_row(V[i][c], p + c * 8 * C::VB);
-                else ld_row(V[i][c], p + c * 8 * C::VB, o != ~0u);
+                ld_row(V[i][c], p + c * 8 * C::VB, o != ~0u);
             }
         }
     };
@@ -428,8 +437,8 @@ __global__ void __launch_bounds__(kPaThreads, (Tile<D, F16Q, E4M3, HG>::CTAS)) p
     uint32_t off = key_offset(a, ask(w, j));
     KeyAt next = ask(w, j + C::STEP);
     uint32_t valid = valid_of(off);
-    load_K(off, valid == kFull);
-    load_V(off, valid == kFull);
+    load_K(off);
+    load_V(off);
     load_Q(w);
 
     while (true) {
@@ -489,8 +498,8 @@ __global__ void __launch_bounds__(kPaThreads, (Tile<D, F16Q, E4M3, HG>::CTAS)) p
             const bool more = s + 1 < w.hi;
             if (valid == 0u) {                        // a short item: nothing for this warp
                 if (more) {
-                    load_K(off_next, false);
-                    load_V(off_next, false);
+                    load_K(off_next);
+                    load_V(off_next);
                 }
                 valid = valid_next;
                 continue;
@@ -517,7 +526,7 @@ __global__ void __launch_bounds__(kPaThreads, (Tile<D, F16Q, E4M3, HG>::CTAS)) p
                     for (int hg = 0; hg < HG; ++hg) mma<C::F16>(S[i][hg], a0, a1, a2, a3, qf[hg][ks][0], qf[hg][ks][1]);
                 }
             }
-            if (more) load_K(off_next, valid_next == kFull);
+            if (more) load_K(off_next);
 
             // running maximum and sum of two heads (four for 16) a lane
 #pragma unroll
@@ -610,15 +619,15 @@ __global__ void __launch_bounds__(kPaThreads, (Tile<D, F16Q, E4M3, HG>::CTAS)) p
                             if (!C::F16) mma<C::F16>(acc, a0, a1, a2, a3, pl[i][hg][0], pl[i][hg][1]);
                         }
                     }
-            if (more) load_V(off_next, valid_next == kFull);
+            if (more) load_V(off_next);
             valid = valid_next;
         }
 
         auto request = [&] {
             off = key_offset(a, x_key);
             valid = valid_of(off);
-            load_K(off, valid == kFull);
-            load_V(off, valid == kFull);
+            load_K(off);
+            load_V(off);
             load_Q(x);
             j = first_key(x);
             next = ask(x, j + C::STEP);
@@ -683,33 +692,33 @@ __global__ void __launch_bounds__(kPaThreads, (Tile<D, F16Q, E4M3, HG>::CTAS)) p
             const int first = p.first, n = p.n, mine = (int)blockIdx.x - first;
             // counts this CTA in; true for the last of n
             auto arrive = [&](int32_t* ticket, int of) {
-                __threadfence();
                 __syncthreads();
                 if (tid == 0) {
+                    __threadfence();                         // of the whole CTA's results: they came before the barrier
                     last_flag = atomicAdd(ticket, 1) == of - 1;
                     if (last_flag) *ticket = 0;
+                    __threadfence();
                 }
                 __syncthreads();
-                const bool last = last_flag;
-                if (last) __threadfence();
-                return last;
+                return last_flag != 0;
             };
             // counters: of the item; of its first group; of a later group, by the group's first CTA (which may also begin an item)
             int32_t* tickets = a.tickets + first;
             if (n <= kPaJoin) {
-                if (arrive(tickets, n)) join_pieces<D, F16Q>(a.part, first, 0, 1, n, rows, sO, &out);
+                if (arrive(tickets, n)) join_pieces<D, F16Q>(a.part, first, 0, 1, n, rows, &out);
             } else {
                 // levels: groups of kPaJoin pieces, then their results
                 const int group = mine / kPaJoin, groups = (n + kPaJoin - 1) / kPaJoin, p0 = group * kPaJoin;
                 const int count = min(kPaJoin, n - p0);
                 if (arrive(tickets + kPaTicketRow * (group == 0 ? 1 : 2) + p0, count)) {
-                    join_pieces<D, F16Q>(a.part, first, p0, 1, count, rows, sO, nullptr);
+                    join_pieces<D, F16Q>(a.part, first, p0, 1, count, rows, nullptr);
                     if (arrive(tickets, groups)) {
                         // beyond kPaJoin^2 pieces one more level, by this CTA alone
                         for (int q0 = 0; groups > kPaJoin && q0 < groups; q0 += kPaJoin)
-                            join_pieces<D, F16Q>(a.part, first, q0 * kPaJoin, kPaJoin, min(kPaJoin, groups - q0), rows, sO, nullptr);
+                            join_pieces<D, F16Q>(a.part, first, q0 * kPaJoin, kPaJoin, min(kPaJoin, groups - q0), rows, nullptr);
                         const int by = groups > kPaJoin ? kPaJoin * kPaJoin : kPaJoin;
-                        join_pieces<D, F16Q>(a.part, first, 0, by, (n + by - 1) / by, rows, sO, &out);
+                        __syncthreads();
+                        join_pieces<D, F16Q>(a.part, first, 0, by, (n + by - 1) / by, rows, &out);
                     }
                 }
             }

@@ -28,7 +28,7 @@ PAFU_HD uint64_t div_u64(uint64_t a, uint64_t b) {             // the 32-bit div
 }
 
 constexpr int kPaItemCost = 1;        // what an item costs beside its steps, in steps
-constexpr int kPaMinShare = 4;        // steps and item costs that a CTA takes at least (where there are as many)
+constexpr int kPaMinShare = 2;        // steps and item costs that a CTA takes at least (where there are as many)
 
 // The items of a call laid end to end, each of cost = steps + kPaItemCost, in `n` shares: cut k (0 to n) lies at all * k / n, and
 // moves to the end of its item where it would leave fewer than `snap` steps of the item on that side.
@@ -43,7 +43,7 @@ PAFU_HD PagedCuts paged_cuts(uint64_t all, uint32_t grid) {
     const uint64_t n = div_u64(all, kPaMinShare);
     c.n = n < 1 ? 1u : n < grid ? (uint32_t)n : grid;
     const uint64_t share = div_u64(all, c.n);
-    c.snap = share < 4 ? 1 : share <= 8 ? (int32_t)(share / 2) : share < 32 ? 2 : 1;
+    c.snap = share < 32 ? 2 : 1;
     return c;
 }
 PAFU_HD uint64_t paged_cut(const PagedCuts& c, uint32_t k) { return div_u64(c.all * k, c.n); }

@@ -15,7 +15,9 @@ namespace {
 // the entries to write; an entry finds its request by a binary search in the threads' sums and a walk through one stretch.
 // That keeps a step one launch: nothing a CTA reads is written by another (a request that grows only gets table
 // entries behind those that are read, the free list only entries above its top), apart from the lengths and the free count,
-// which may be updated in place; the CTA that counts itself out last writes those.  A step moves a few KB: latency bounds it.
+// which may be updated in place; the CTA that counts itself out last writes those.  A step moves a few KB to MB: the
+// trips to memory that follow one another bound it, so a thread issues its loads before it uses the first, and in a
+// long step takes eight neighbouring tokens, which mostly share a request and a page.
 constexpr int kTabThreads = 512;
 
 struct TablesArgs {
@@ -52,6 +54,8 @@ __device__ __forceinline__ int32_t pages_of(const FastDiv& page, int32_t len) {
     return len <= 0 ? 0 : (int32_t)div_by((uint32_t)(len - 1), page) + 1;
 }
 
+// PER: neighbouring tokens a thread
+template <int PER>
 __global__ void __launch_bounds__(kTabThreads) paged_tables_kernel(const TablesArgs a) {
     __shared__ int64_t s_need[kTabThreads + 1], s_back[kTabThreads + 1], s_tok[kTabThreads + 1];
     __shared__ Sums s_warp[kTabThreads / 32];
@@ -59,22 +63,27 @@ __global__ void __launch_bounds__(kTabThreads) paged_tables_kernel(const TablesA
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     grid_dep_wait();
     const int per = (a.n_requests + kTabThreads - 1) / kTabThreads;
-    auto lens = [&](int r) {
-        Lens x;
-        x.old_len = ld_index(a.len_old + r);
-        x.new_len = ld_index(a.len_new + r);
-        x.have = pages_of(a.page, x.old_len);
-        x.want = pages_of(a.page, x.new_len);
-        return x;
+    auto lens_of = [&](int32_t before, int32_t after) {
+        return Lens{before, after, pages_of(a.page, before), pages_of(a.page, after)};
     };
+    auto lens = [&](int r) { return lens_of(ld_index(a.len_old + r), ld_index(a.len_new + r)); };
     const int32_t F = ld_index(a.n_free);
     const int r0 = min(tid * per, a.n_requests), r1 = min(r0 + per, a.n_requests);
     Sums mine{0, 0, 0};
     bool bad = F < 0 || (uint32_t)F > a.n_pages;
-    for (int r = r0; r < r1; ++r) {
-        const Lens x = lens(r);
-        bad |= x.old_len < 0 || x.new_len < 0 || x.have > a.max_pages || x.want > a.max_pages;
-        mine = mine + Sums{x.need(), x.back(), x.tokens()};
+    for (int r = r0; r < r1; r += 4) {
+        int32_t before[4], after[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            before[i] = r + i < r1 ? ld_index(a.len_old + r + i) : 0;
+            after[i] = r + i < r1 ? ld_index(a.len_new + r + i) : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const Lens x = lens_of(before[i], after[i]);
+            bad |= x.old_len < 0 || x.new_len < 0 || x.have > a.max_pages || x.want > a.max_pages;
+            mine = mine + Sums{x.need(), x.back(), x.tokens()};
+        }
     }
     Sums inc = mine;
 #pragma unroll
@@ -92,11 +101,6 @@ __global__ void __launch_bounds__(kTabThreads) paged_tables_kernel(const TablesA
     s_need[tid] = before.need;
     s_back[tid] = before.back;
     s_tok[tid] = before.tokens;
-    if (tid == 0) {
-        s_need[kTabThreads] = all.need;
-        s_back[kTabThreads] = all.back;
-        s_tok[kTabThreads] = all.tokens;
-    }
     __syncthreads();
     // all or nothing: every page must exist, every token have a place in the slot map
     const int64_t height = (int64_t)F + all.back;               // of the stack, with what is given back on top
@@ -104,7 +108,7 @@ __global__ void __launch_bounds__(kTabThreads) paged_tables_kernel(const TablesA
     const bool ok = !bad && !short_of && height - all.need <= (int64_t)a.n_pages;
     if (!ok && blockIdx.x == 0 && tid == 0) *a.status = bad || !short_of ? PAFU_ERR_BAD_PAGE : PAFU_ERR_NO_PAGES;
 
-    // request that holds number i of a sum, and the sum before it
+    // request that holds number i of a sum; returns i's place among the request's own
     auto find = [&](const int64_t* sums, int64_t i, auto value, int* request, Lens* x) {
         int lo = 0, hi = kTabThreads - 1;                        // last thread whose sum is <= i
         while (lo < hi) {
@@ -125,42 +129,67 @@ __global__ void __launch_bounds__(kTabThreads) paged_tables_kernel(const TablesA
     auto need_of = [](const Lens& x) { return x.need(); };
     auto back_of = [](const Lens& x) { return x.back(); };
     auto tokens_of = [](const Lens& x) { return x.tokens(); };
-    // entry v of the stack: the free list, then the pages given back in the order of requests and columns
-    auto stack = [&](int64_t v) -> int32_t {
-        if (v < F) return ld_index(a.free_list + v);
+    // where entry v of the stack lies: in the free list, then the pages given back in the order of requests and columns
+    auto stack = [&](int64_t v) -> const int32_t* {
+        if (v < F) return a.free_list + v;
         int r;
         Lens x;
         const int64_t i = find(s_back, v - F, back_of, &r, &x);
-        return ld_index(a.table + (int64_t)r * a.max_pages + x.want + i);
+        return a.table + (int64_t)r * a.max_pages + x.want + i;
     };
-    const int64_t step = (int64_t)gridDim.x * kTabThreads, start = (int64_t)blockIdx.x * kTabThreads + tid;
-    if (ok) {
-        for (int64_t i = start; i < all.need; i += step) {
+    // table entries, entries of the free list, and the slot map side by side: no thread does one after the other
+    const int64_t pages = ok ? all.need : 0, pushed = ok ? max(height - all.need - F, (int64_t)0) : 0;
+    const int64_t jobs = pages + pushed + (a.n_slots + PER - 1) / PER;
+    for (int64_t job = (int64_t)blockIdx.x * kTabThreads + tid; job < jobs; job += (int64_t)gridDim.x * kTabThreads) {
+        if (job < pages) {
             int r;
             Lens x;
-            const int64_t c = find(s_need, i, need_of, &r, &x);
-            a.table[(int64_t)r * a.max_pages + x.have + c] = stack(height - 1 - i);
-        }
-        for (int64_t v = F + start; v < height - all.need; v += step) a.free_list[v] = stack(v);
-    }
-    for (int64_t j = start; j < a.n_slots; j += step) {
-        int64_t slot = -1;
-        if (ok && j < all.tokens) {
-            int r;
-            Lens x;
-            const int64_t pos = find(s_tok, j, tokens_of, &r, &x) + x.old_len;
-            const int32_t p = (int32_t)div_by((uint32_t)pos, a.page);
-            int32_t page;
-            if (p < x.have) {
-                page = ld_index(a.table + (int64_t)r * a.max_pages + p);
-            } else {
-                int64_t needed = s_need[r / per];                // pages needed by the requests before r
+            const int64_t c = find(s_need, job, need_of, &r, &x);
+            a.table[(int64_t)r * a.max_pages + x.have + c] = ld_index(stack(height - 1 - job));
+        } else if (job < pages + pushed) {
+            const int64_t v = F + job - pages;
+            a.free_list[v] = ld_index(stack(v));
+        } else {
+            const int64_t j0 = (job - pages - pushed) * PER;
+            const int32_t* from[PER];                            // the tokens' pages
+            int32_t place[PER];
+            int r = 0;
+            Lens x{0, 0, 0, 0};
+            int64_t pos = 0, needed = 0;
+            if (ok && j0 < all.tokens) {
+                pos = find(s_tok, j0, tokens_of, &r, &x) + x.old_len;
+                needed = s_need[r / per];                        // pages needed by the requests before r
                 for (int q = r / per * per; q < r; ++q) needed += lens(q).need();
-                page = stack(height - 1 - (needed + p - x.have));
             }
-            slot = (int64_t)page * a.page.d + (pos - (int64_t)p * a.page.d);
+            int32_t last = -1;
+#pragma unroll
+            for (int k = 0; k < PER; ++k) {
+                if (!ok || j0 + k >= all.tokens) {
+                    from[k] = nullptr;
+                    place[k] = 0;
+                    continue;
+                }
+                while (pos >= x.new_len) {                       // the next request with new tokens
+                    needed += x.need();
+                    x = lens(++r);
+                    pos = x.old_len;
+                    last = -1;
+                }
+                const int32_t p = (int32_t)div_by((uint32_t)pos, a.page);
+                if (k > 0 && p == last) from[k] = from[k - 1];
+                else if (p < x.have) from[k] = a.table + (int64_t)r * a.max_pages + p;
+                else from[k] = stack(height - 1 - (needed + p - x.have));
+                last = p;
+                place[k] = (int32_t)(pos - (int64_t)p * a.page.d);
+                ++pos;
+            }
+            int32_t page[PER];
+#pragma unroll
+            for (int k = 0; k < PER; ++k) page[k] = from[k] != nullptr ? ld_index(from[k]) : 0;
+#pragma unroll
+            for (int k = 0; k < PER; ++k)
+                if (j0 + k < a.n_slots) a.slots[j0 + k] = from[k] != nullptr ? (int64_t)page[k] * a.page.d + place[k] : -1;
         }
-        a.slots[j] = slot;
     }
     if (blockIdx.x == 0) {
         int64_t at = before.tokens;
@@ -171,20 +200,21 @@ __global__ void __launch_bounds__(kTabThreads) paged_tables_kernel(const TablesA
         if (tid == 0) a.cu_new[a.n_requests] = ok ? (int32_t)all.tokens : 0;
     }
     // what may be updated in place, once every CTA has read it
-    __threadfence();
     __syncthreads();
-    if (tid == 0) s_last = atomicAdd(a.ticket, 1) == (int)gridDim.x - 1;
-    __syncthreads();
-    if (s_last) {
-        for (int r = tid; r < a.n_requests; r += kTabThreads) {
-            const int32_t o = ld_index(a.len_old + r), n = ld_index(a.len_new + r);
-            a.len_out[r] = ok ? n : o;
-        }
+    if (gridDim.x > 1) {
         if (tid == 0) {
-            *a.n_free_out = ok ? (int32_t)(height - all.need) : F;
-            *a.ticket = 0;
+            __threadfence();
+            s_last = atomicAdd(a.ticket, 1) == (int)gridDim.x - 1;
+            if (s_last) *a.ticket = 0;
         }
+        __syncthreads();
+        if (!s_last) return;
     }
+    for (int r = tid; r < a.n_requests; r += kTabThreads) {
+        const int32_t o = ld_index(a.len_old + r), n = ld_index(a.len_new + r);
+        a.len_out[r] = ok ? n : o;
+    }
+    if (tid == 0) *a.n_free_out = ok ? (int32_t)(height - all.need) : F;
 }
 
 // ---------------------------------------------------------------------------------- append
@@ -288,10 +318,12 @@ pafu_status launch_paged_tables(const pafu_paged_cache& c, const int32_t* len_ol
     a.cu_new = cu_new;
     a.status = static_cast<int32_t*>(ws) + kStatusWordPaged;
     a.ticket = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + kWsHeaderBytes) + kPagedTickets - 1;
-    // a CTA for every 2048 places of the slot map
-    const int64_t want = (n_slots + 4 * kTabThreads - 1) / (4 * kTabThreads), most = device_sm_count();
-    const int64_t grid = want < 1 ? 1 : want < most ? want : most;
-    return cuda_ok(launch_dependent(paged_tables_kernel, dim3((unsigned)grid), dim3(kTabThreads), 0, stream, 1, a));
+    // Eight tokens a thread once one each would take more than 32 CTAs: a step of 2000 requests and 360000 tokens takes 9 us so
+    // and 19 with one, one of 256 single tokens 4.3 and 5.5.
+    const bool runs = n_slots > 32 * kTabThreads;
+    const int64_t jobs = (runs ? n_slots / 8 : n_slots) + c.n_requests / 4, want = (jobs + kTabThreads - 1) / kTabThreads;
+    const int64_t most = device_sm_count(), grid = want < 1 ? 1 : want < most ? want : most;
+    return cuda_ok(launch_dependent(runs ? paged_tables_kernel<8> : paged_tables_kernel<1>, dim3((unsigned)grid), dim3(kTabThreads), 0, stream, 1, a));
 }
 
 pafu_status launch_paged_append(const pafu_paged_cache& c, const void* Kn, const void* Vn, int64_t ld_token, int64_t ld_head,

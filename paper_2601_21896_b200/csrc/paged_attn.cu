@@ -61,21 +61,29 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 
-// 16 (8) bytes of a row, or zeros.  (Predicated in one piece: as a branch, or with a second copy of the loads for whole tiles, the loop
-// over the keys runs 4 to 8 % longer.)
-__device__ __forceinline__ void ld_row(uint32_t (&w)[4], const char* p, bool ok) {
-    w[0] = w[1] = w[2] = w[3] = 0u;
-    asm volatile(
-        "{\n\t.reg .pred P;\n\tsetp.ne.b32 P, %5, 0;\n\t"
-        "@P ld.global.nc.L1::no_allocate.L2::128B.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
-        : "+r"(w[0]), "+r"(w[1]), "+r"(w[2]), "+r"(w[3]) : "l"(p), "r"((int)ok) : "memory");
-}
-__device__ __forceinline__ void ld_row(uint32_t (&w)[2], const char* p, bool ok) {
-    w[0] = w[1] = 0u;
-    asm volatile(
-        "{\n\t.reg .pred P;\n\tsetp.ne.b32 P, %3, 0;\n\t"
-        "@P ld.global.nc.L1::no_allocate.L2::128B.v2.u32 {%0, %1}, [%2];\n\t}"
-        : "+r"(w[0]), "+r"(w[1]) : "l"(p), "r"((int)ok) : "memory");
+// 16 (8) bytes of a row, or zeros.  Predicated in one piece: as a branch, or with a second copy of the loads for whole tiles, the loop
+// over the keys runs 4 to 8 % longer.  Rows of 64 bytes are fetched as such: two heads of a token share a 128-byte line, but
+// come at different times (16 heads of 64 in 8 bits, 1.08 GB: 354 us with whole lines, 313 so).
+#define PAFU_LD_ROW(HINT)                                                                                       \
+    __device__ __forceinline__ void ld_row##HINT(uint32_t (&w)[4], const char* p, bool ok) {                    \
+        w[0] = w[1] = w[2] = w[3] = 0u;                                                                         \
+        asm volatile("{\n\t.reg .pred P;\n\tsetp.ne.b32 P, %5, 0;\n\t"                                          \
+                     "@P ld.global.nc.L1::no_allocate.L2::" #HINT "B.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"       \
+                     : "+r"(w[0]), "+r"(w[1]), "+r"(w[2]), "+r"(w[3]) : "l"(p), "r"((int)ok) : "memory");       \
+    }                                                                                                           \
+    __device__ __forceinline__ void ld_row##HINT(uint32_t (&w)[2], const char* p, bool ok) {                    \
+        w[0] = w[1] = 0u;                                                                                       \
+        asm volatile("{\n\t.reg .pred P;\n\tsetp.ne.b32 P, %3, 0;\n\t"                                          \
+                     "@P ld.global.nc.L1::no_allocate.L2::" #HINT "B.v2.u32 {%0, %1}, [%2];\n\t}"               \
+                     : "+r"(w[0]), "+r"(w[1]) : "l"(p), "r"((int)ok) : "memory");                               \
+    }
+PAFU_LD_ROW(64)
+PAFU_LD_ROW(128)
+#undef PAFU_LD_ROW
+template <int ROW, int N>
+__device__ __forceinline__ void ld_row(uint32_t (&w)[N], const char* p, bool ok) {
+    if (ROW <= 64) ld_row64(w, p, ok);
+    else ld_row128(w, p, ok);
 }
 
 template <bool F16>
@@ -138,7 +146,9 @@ __device__ __forceinline__ Kept kept_of(const PagedAttnArgs& a, int32_t T) {
 template <int D, bool F16Q, bool E4M3, int HG>
 struct Tile {
     static constexpr int ES = E4M3 ? 1 : 2;
-    static constexpr int KT = D * ES >= 256 ? 16 : 32;            // keys of a warp's tile: 4 to 8 KB of K and V in flight a warp
+    // Keys of a warp's tile: 4 to 8 KB of K and V in flight a warp.  (Half as many: no difference at rows of 256 bytes, which the bytes
+    // bound; 6 to 28 % longer at the others, which issue more instructions a byte.)
+    static constexpr int KT = D * ES >= 256 ? 16 : 32;
     static constexpr int KR = KT / 8;                             // key rows that a lane has a part of
     static constexpr int KW = D * ES / 16;                        // words of each
     static constexpr int VR = KT / 4;                             // value rows
@@ -382,7 +392,7 @@ __global__ void __launch_bounds__(kPaThreads, (Tile<D, F16Q, E4M3, HG>::CTAS)) p
             const char* p = a.pool.K + (uint64_t)o * 16 + t * 16;
 #pragma unroll
             for (int c = 0; c < C::KW / 4; ++c) {
-                ld_row(K[i][c], p + c * 64, o != ~0u);
+                ld_row<D * C::ES>(K[i][c], p + c * 64, o != ~0u);
             }
         }
     };
@@ -393,7 +403,7 @@ __global__ void __launch_bounds__(kPaThreads, (Tile<D, F16Q, E4M3, HG>::CTAS)) p
             const char* p = a.pool.V + (uint64_t)o * 16 + g * C::VB;
 #pragma unroll
             for (int c = 0; c < C::VC; ++c) {
-                ld_row(V[i][c], p + c * 8 * C::VB, o != ~0u);
+                ld_row<D * C::ES>(V[i][c], p + c * 8 * C::VB, o != ~0u);
             }
         }
     };
@@ -422,7 +432,7 @@ __global__ void __launch_bounds__(kPaThreads, (Tile<D, F16Q, E4M3, HG>::CTAS)) p
 #pragma unroll
                 for (int h = 0; h < PER / 8; ++h) {
                     uint32_t q[4];
-                    ld_row(q, p + h * 16, have);
+                    ld_row<D * 2>(q, p + h * 16, have);
                     const int ks = c * (PER / 4) + h * 2;
                     qf[hg][ks][0] = q[0];
                     qf[hg][ks][1] = q[1];
@@ -477,6 +487,7 @@ __global__ void __launch_bounds__(kPaThreads, (Tile<D, F16Q, E4M3, HG>::CTAS)) p
                         qf[hg][ks][i] = pack2<true>(v.x * f, v.y * f);
                     }
             }
+            c_row = fmaxf(c_row, 1e-37f);             // -inf times it stays -inf: a scale of 0 makes all logits equal
             c_col[hg][0] = __shfl_sync(0xffffffffu, c_row, 8 * t);
             c_col[hg][1] = __shfl_sync(0xffffffffu, c_row, 8 * t + 4);
         }
@@ -528,13 +539,6 @@ __global__ void __launch_bounds__(kPaThreads, (Tile<D, F16Q, E4M3, HG>::CTAS)) p
             }
             if (more) load_K(off_next);
 
-            // running maximum and sum of two heads (four for 16) a lane
-#pragma unroll
-            for (int i = 0; i < C::KT / 16; ++i)
-#pragma unroll
-                for (int hg = 0; hg < HG; ++hg)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) S[i][hg][k] *= c_col[hg][k & 1];
             if (valid != kFull) {
 #pragma unroll
                 for (int i = 0; i < C::KT / 16; ++i)
@@ -557,15 +561,15 @@ __global__ void __launch_bounds__(kPaThreads, (Tile<D, F16Q, E4M3, HG>::CTAS)) p
                     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
                     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
                     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-                    const float base = top == -INFINITY ? 0.f : top;
-                    f[hg][k] = ex2(m[hg][k] - base);
+                    const float c = c_col[hg][k], base = top == -INFINITY ? 0.f : top * c;
+                    f[hg][k] = ex2(fmaf(m[hg][k], c, -base));
                     moved |= top != m[hg][k];
                     m[hg][k] = top;
                     float sum = 0.f;
 #pragma unroll
                     for (int i = 0; i < C::KT / 16; ++i) {
-                        S[i][hg][k] = ex2(S[i][hg][k] - base);
-                        S[i][hg][k + 2] = ex2(S[i][hg][k + 2] - base);
+                        S[i][hg][k] = ex2(fmaf(S[i][hg][k], c, -base));
+                        S[i][hg][k + 2] = ex2(fmaf(S[i][hg][k + 2], c, -base));
                         sum += S[i][hg][k] + S[i][hg][k + 2];
                     }
                     l[hg][k] = l[hg][k] * f[hg][k] + sum;
@@ -647,7 +651,7 @@ __global__ void __launch_bounds__(kPaThreads, (Tile<D, F16Q, E4M3, HG>::CTAS)) p
                 sum += __shfl_xor_sync(0xffffffffu, sum, 16);
                 const int row = hg * 8 + 2 * t + k;
                 if (g == 0) {
-                    sM[warp * C::ROWS + row] = m[hg][k];
+                    sM[warp * C::ROWS + row] = m[hg][k] * c_col[hg][k];
                     sL[warp * C::ROWS + row] = sum;
                 }
                 if (row < rows) {

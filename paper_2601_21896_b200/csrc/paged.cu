@@ -10,15 +10,18 @@ namespace {
 
 // ---------------------------------------------------------------------------------- tables
 // From the lengths before and after a step: which pages each request gives back and gets, where its new tokens go.
-// All of it follows from three prefix sums over the requests (pages needed, pages given back, new tokens), so every CTA computes
-// them for itself - each thread sums a stretch of requests, one scan of the threads' sums - and then takes its part of
-// the entries to write; an entry finds its request by a binary search in the threads' sums and a walk through one stretch.
+// All of it follows from prefix sums over the requests (pages needed, pages given back, new tokens, and the runs below), so every
+// CTA computes them for itself - each thread sums a stretch of requests, one scan of the threads' sums - and then takes its part of
+// what there is to write.  The unit is a run: new tokens of a request that lie in the same sixteenth-token stretch of a page.  A
+// thread finds its run by a binary search in the threads' sums and a walk through one stretch of requests, looks up the page once,
+// writes the run's slots, and the table entry where the run begins a new page.
 // That keeps a step one launch: nothing a CTA reads is written by another (a request that grows only gets table
 // entries behind those that are read, the free list only entries above its top), apart from the lengths and the free count,
 // which may be updated in place; the CTA that counts itself out last writes those.  A step moves a few KB to MB: the
-// trips to memory that follow one another bound it, so a thread issues its loads before it uses the first, and in a
-// long step takes eight neighbouring tokens, which mostly share a request and a page.
+// trips to memory and the searches that follow one another bound it.  2000 requests with 360000 new tokens: 19 us with a search
+// and a lookup for every token.
 constexpr int kTabThreads = 512;
+constexpr int kTabRun = 16;           // tokens of a run, at most
 
 struct TablesArgs {
     int32_t* table;
@@ -46,30 +49,37 @@ struct Lens {
 };
 
 struct Sums {
-    int64_t need, back, tokens;
+    int64_t need, back, tokens, runs;
 };
-__device__ __forceinline__ Sums operator+(const Sums& a, const Sums& b) { return Sums{a.need + b.need, a.back + b.back, a.tokens + b.tokens}; }
+__device__ __forceinline__ Sums operator+(const Sums& a, const Sums& b) {
+    return Sums{a.need + b.need, a.back + b.back, a.tokens + b.tokens, a.runs + b.runs};
+}
 
 __device__ __forceinline__ int32_t pages_of(const FastDiv& page, int32_t len) {
     return len <= 0 ? 0 : (int32_t)div_by((uint32_t)(len - 1), page) + 1;
 }
 
-// PER: neighbouring tokens a thread
-template <int PER>
 __global__ void __launch_bounds__(kTabThreads) paged_tables_kernel(const TablesArgs a) {
-    __shared__ int64_t s_need[kTabThreads + 1], s_back[kTabThreads + 1], s_tok[kTabThreads + 1];
+    __shared__ uint32_t s_back[kTabThreads], s_runs[kTabThreads], s_need[kTabThreads], s_tok[kTabThreads];
     __shared__ Sums s_warp[kTabThreads / 32];
     __shared__ int32_t s_last;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int32_t per_page = (int32_t)((a.page.d + kTabRun - 1) / kTabRun);         // runs of a full page
     grid_dep_wait();
     const int per = (a.n_requests + kTabThreads - 1) / kTabThreads;
     auto lens_of = [&](int32_t before, int32_t after) {
         return Lens{before, after, pages_of(a.page, before), pages_of(a.page, after)};
     };
     auto lens = [&](int r) { return lens_of(ld_index(a.len_old + r), ld_index(a.len_new + r)); };
+    // number of the run that position `pos` is in, counted from the request's first position
+    auto run_at = [&](int32_t pos) {
+        const int32_t p = (int32_t)div_by((uint32_t)pos, a.page);
+        return p * per_page + (pos - p * (int32_t)a.page.d) / kTabRun;
+    };
+    auto runs_of = [&](const Lens& x) { return x.tokens() > 0 ? run_at(x.new_len - 1) - run_at(x.old_len) + 1 : 0; };
     const int32_t F = ld_index(a.n_free);
     const int r0 = min(tid * per, a.n_requests), r1 = min(r0 + per, a.n_requests);
-    Sums mine{0, 0, 0};
+    Sums mine{0, 0, 0, 0};
     bool bad = F < 0 || (uint32_t)F > a.n_pages;
     for (int r = r0; r < r1; r += 4) {
         int32_t before[4], after[4];
@@ -81,114 +91,90 @@ __global__ void __launch_bounds__(kTabThreads) paged_tables_kernel(const TablesA
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const Lens x = lens_of(before[i], after[i]);
-            bad |= x.old_len < 0 || x.new_len < 0 || x.have > a.max_pages || x.want > a.max_pages;
-            mine = mine + Sums{x.need(), x.back(), x.tokens()};
+            const bool wrong = x.old_len < 0 || x.new_len < 0 || x.have > a.max_pages || x.want > a.max_pages;
+            bad |= wrong;
+            if (!wrong) mine = mine + Sums{x.need(), x.back(), x.tokens(), runs_of(x)};
         }
     }
     Sums inc = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const Sums v{__shfl_up_sync(0xffffffffu, inc.need, o), __shfl_up_sync(0xffffffffu, inc.back, o), __shfl_up_sync(0xffffffffu, inc.tokens, o)};
+        const Sums v{__shfl_up_sync(0xffffffffu, inc.need, o), __shfl_up_sync(0xffffffffu, inc.back, o),
+                     __shfl_up_sync(0xffffffffu, inc.tokens, o), __shfl_up_sync(0xffffffffu, inc.runs, o)};
         if (lane >= o) inc = inc + v;
     }
     if (lane == 31) s_warp[warp] = inc;
     bad = __syncthreads_or(bad);
-    Sums all{0, 0, 0}, before{inc.need - mine.need, inc.back - mine.back, inc.tokens - mine.tokens};
+    Sums all{0, 0, 0, 0}, before{inc.need - mine.need, inc.back - mine.back, inc.tokens - mine.tokens, inc.runs - mine.runs};
     for (int w = 0; w < kTabThreads / 32; ++w) {
         if (w < warp) before = before + s_warp[w];
         all = all + s_warp[w];
     }
-    s_need[tid] = before.need;
-    s_back[tid] = before.back;
-    s_tok[tid] = before.tokens;
+    s_need[tid] = (uint32_t)before.need;
+    s_back[tid] = (uint32_t)before.back;
+    s_tok[tid] = (uint32_t)before.tokens;
+    s_runs[tid] = (uint32_t)before.runs;
     __syncthreads();
     // all or nothing: every page must exist, every token have a place in the slot map
     const int64_t height = (int64_t)F + all.back;               // of the stack, with what is given back on top
     const bool short_of = all.need > height || all.tokens > a.n_slots;
+    // (a step that passes gives back fewer than 2^32 pages and has fewer than 2^31 of everything else)
     const bool ok = !bad && !short_of && height - all.need <= (int64_t)a.n_pages;
     if (!ok && blockIdx.x == 0 && tid == 0) *a.status = bad || !short_of ? PAFU_ERR_BAD_PAGE : PAFU_ERR_NO_PAGES;
 
-    // request that holds number i of a sum; returns i's place among the request's own
-    auto find = [&](const int64_t* sums, int64_t i, auto value, int* request, Lens* x) {
-        int lo = 0, hi = kTabThreads - 1;                        // last thread whose sum is <= i
+    // the last thread whose sum is <= i
+    auto stretch = [&](const uint32_t* sums, uint32_t i) {
+        int lo = 0, hi = kTabThreads - 1;
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
             if (sums[mid] <= i) lo = mid;
             else hi = mid - 1;
         }
-        int64_t at = sums[lo];
-        int r = lo * per;
-        *x = lens(r);
-        while (i >= at + value(*x)) {
-            at += value(*x);
-            *x = lens(++r);
-        }
-        *request = r;
-        return i - at;
+        return lo;
     };
-    auto need_of = [](const Lens& x) { return x.need(); };
-    auto back_of = [](const Lens& x) { return x.back(); };
-    auto tokens_of = [](const Lens& x) { return x.tokens(); };
     // where entry v of the stack lies: in the free list, then the pages given back in the order of requests and columns
     auto stack = [&](int64_t v) -> const int32_t* {
         if (v < F) return a.free_list + v;
-        int r;
-        Lens x;
-        const int64_t i = find(s_back, v - F, back_of, &r, &x);
+        const int at = stretch(s_back, (uint32_t)(v - F));
+        uint32_t i = (uint32_t)(v - F) - s_back[at];
+        int r = at * per;
+        Lens x = lens(r);
+        while (i >= (uint32_t)x.back()) {
+            i -= x.back();
+            x = lens(++r);
+        }
         return a.table + (int64_t)r * a.max_pages + x.want + i;
     };
-    // table entries, entries of the free list, and the slot map side by side: no thread does one after the other
-    const int64_t pages = ok ? all.need : 0, pushed = ok ? max(height - all.need - F, (int64_t)0) : 0;
-    const int64_t jobs = pages + pushed + (a.n_slots + PER - 1) / PER;
+    // runs, entries of the free list, and the slot map's end side by side: no thread does one after the other
+    const int64_t runs = ok ? all.runs : 0, pushed = ok ? max(height - all.need - F, (int64_t)0) : 0;
+    const int64_t filled = ok ? all.tokens : 0, jobs = runs + pushed + (a.n_slots - filled + kTabRun - 1) / kTabRun;
     for (int64_t job = (int64_t)blockIdx.x * kTabThreads + tid; job < jobs; job += (int64_t)gridDim.x * kTabThreads) {
-        if (job < pages) {
-            int r;
-            Lens x;
-            const int64_t c = find(s_need, job, need_of, &r, &x);
-            a.table[(int64_t)r * a.max_pages + x.have + c] = ld_index(stack(height - 1 - job));
-        } else if (job < pages + pushed) {
-            const int64_t v = F + job - pages;
+        if (job < runs) {
+            const int at = stretch(s_runs, (uint32_t)job);
+            int32_t i = (int32_t)((uint32_t)job - s_runs[at]);
+            uint32_t needed = s_need[at], token = s_tok[at];
+            int r = at * per;
+            Lens x = lens(r);
+            while (i >= runs_of(x)) {
+                i -= runs_of(x);
+                needed += x.need();
+                token += x.tokens();
+                x = lens(++r);
+            }
+            const int32_t run = run_at(x.old_len) + i, p = run / per_page, first = p * (int32_t)a.page.d + (run - p * per_page) * kTabRun;
+            const int32_t last = min(min(first + kTabRun, (p + 1) * (int32_t)a.page.d), x.new_len), pos = max(first, x.old_len);
+            int32_t* entry = a.table + (int64_t)r * a.max_pages + p;
+            const int32_t page = ld_index(p < x.have ? entry : stack(height - 1 - ((int64_t)needed + p - x.have)));
+            if (p >= x.have && first == p * (int32_t)a.page.d) *entry = page;
+            int64_t slot = (int64_t)page * a.page.d + (pos - p * (int32_t)a.page.d);
+            int64_t* to = a.slots + token + (pos - x.old_len);
+            for (int k = 0; k < last - pos; ++k) to[k] = slot + k;
+        } else if (job < runs + pushed) {
+            const int64_t v = F + job - runs;
             a.free_list[v] = ld_index(stack(v));
         } else {
-            const int64_t j0 = (job - pages - pushed) * PER;
-            const int32_t* from[PER];                            // the tokens' pages
-            int32_t place[PER];
-            int r = 0;
-            Lens x{0, 0, 0, 0};
-            int64_t pos = 0, needed = 0;
-            if (ok && j0 < all.tokens) {
-                pos = find(s_tok, j0, tokens_of, &r, &x) + x.old_len;
-                needed = s_need[r / per];                        // pages needed by the requests before r
-                for (int q = r / per * per; q < r; ++q) needed += lens(q).need();
-            }
-            int32_t last = -1;
-#pragma unroll
-            for (int k = 0; k < PER; ++k) {
-                if (!ok || j0 + k >= all.tokens) {
-                    from[k] = nullptr;
-                    place[k] = 0;
-                    continue;
-                }
-                while (pos >= x.new_len) {                       // the next request with new tokens
-                    needed += x.need();
-                    x = lens(++r);
-                    pos = x.old_len;
-                    last = -1;
-                }
-                const int32_t p = (int32_t)div_by((uint32_t)pos, a.page);
-                if (k > 0 && p == last) from[k] = from[k - 1];
-                else if (p < x.have) from[k] = a.table + (int64_t)r * a.max_pages + p;
-                else from[k] = stack(height - 1 - (needed + p - x.have));
-                last = p;
-                place[k] = (int32_t)(pos - (int64_t)p * a.page.d);
-                ++pos;
-            }
-            int32_t page[PER];
-#pragma unroll
-            for (int k = 0; k < PER; ++k) page[k] = from[k] != nullptr ? ld_index(from[k]) : 0;
-#pragma unroll
-            for (int k = 0; k < PER; ++k)
-                if (j0 + k < a.n_slots) a.slots[j0 + k] = from[k] != nullptr ? (int64_t)page[k] * a.page.d + place[k] : -1;
+            const int64_t first = filled + (job - runs - pushed) * kTabRun;
+            for (int64_t k = first; k < min(first + kTabRun, a.n_slots); ++k) a.slots[k] = -1;
         }
     }
     if (blockIdx.x == 0) {
@@ -199,11 +185,11 @@ __global__ void __launch_bounds__(kTabThreads) paged_tables_kernel(const TablesA
         }
         if (tid == 0) a.cu_new[a.n_requests] = ok ? (int32_t)all.tokens : 0;
     }
-    // what may be updated in place, once every CTA has read it
+    // What may be updated in place, once every CTA has read it.  (No fence, which would wait for the slots' stores to arrive, 4 us: what was
+    // read has been used, and what the other CTAs wrote is not looked at.)
     __syncthreads();
     if (gridDim.x > 1) {
         if (tid == 0) {
-            __threadfence();
             s_last = atomicAdd(a.ticket, 1) == (int)gridDim.x - 1;
             if (s_last) *a.ticket = 0;
         }
@@ -318,12 +304,10 @@ pafu_status launch_paged_tables(const pafu_paged_cache& c, const int32_t* len_ol
     a.cu_new = cu_new;
     a.status = static_cast<int32_t*>(ws) + kStatusWordPaged;
     a.ticket = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + kWsHeaderBytes) + kPagedTickets - 1;
-    // Eight tokens a thread once one each would take more than 32 CTAs: a step of 2000 requests and 360000 tokens takes 9 us so
-    // and 19 with one, one of 256 single tokens 4.3 and 5.5.
-    const bool runs = n_slots > 32 * kTabThreads;
-    const int64_t jobs = (runs ? n_slots / 8 : n_slots) + c.n_requests / 4, want = (jobs + kTabThreads - 1) / kTabThreads;
-    const int64_t most = device_sm_count(), grid = want < 1 ? 1 : want < most ? want : most;
-    return cuda_ok(launch_dependent(runs ? paged_tables_kernel<8> : paged_tables_kernel<1>, dim3((unsigned)grid), dim3(kTabThreads), 0, stream, 1, a));
+    // About one run a thread in a step that one CTA manages, then about 192 a CTA: their searches are bound by what an SM can issue.
+    const int64_t jobs = n_slots / (kTabRun / 2) + c.n_requests, want = jobs <= kTabThreads ? 1 : (jobs + 191) / 192;
+    const int64_t most = device_sm_count(), grid = want < most ? want : most;
+    return cuda_ok(launch_dependent(paged_tables_kernel, dim3((unsigned)grid), dim3(kTabThreads), 0, stream, 1, a));
 }
 
 pafu_status launch_paged_append(const pafu_paged_cache& c, const void* Kn, const void* Vn, int64_t ld_token, int64_t ld_head,

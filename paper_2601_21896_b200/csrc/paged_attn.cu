@@ -23,6 +23,9 @@
 // item may continue in other CTAs: their fp32 partial results go to the workspace, and the CTA that arrives last
 // (a counter; nothing waits) joins them in a fixed order, so results do not depend on timing; more than 16 pieces are joined
 // in groups of 16 first, by as many CTAs.
+// Where no item has more than two tiles and there are more items than CTAs, a warp takes whole items by itself ("solo"): nothing is
+// joined, no warp is idle on an item of few keys.  12000 items of up to 10 keys of 128: 66.8 us with four warps an item, 24.2 so.  From four
+// tiles on (2400 items of up to 64 keys) both take 24 us, and with fewer items than CTAs four warps are quicker.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math.h>
@@ -194,7 +197,8 @@ struct Cut {
     uint64_t at, item_at;     // the position; where its item begins
     int32_t r, item;
 };
-// A CTA's part of an item: steps [lo, hi) of `steps`; pos: where the item begins, seen from the CTA's first position.
+// A CTA's part of an item: steps [lo, hi) of `steps`; pos: where the item begins, seen from the CTA's first position.  Solo: a warp's
+// item, hi tiles from 0.
 struct Work {
     int32_t r, item, pos, steps, lo, hi;
     Kept kept;
@@ -278,94 +282,44 @@ __device__ __noinline__ void join_pieces(float* parts, int first, int p0, int by
     }
 }
 
-template <int D, bool F16Q, bool E4M3, int HG>
-__global__ void __launch_bounds__(kPaThreads, (Tile<D, F16Q, E4M3, HG>::CTAS)) paged_attn_kernel(const PagedAttnArgs a) {
+// The CTA's items (SOLO: the warp's), one after the other.
+template <int D, bool F16Q, bool E4M3, int HG, bool SOLO>
+__device__ __forceinline__ void attend(const PagedAttnArgs& a, const PagedCuts& plan, const Cut (&cuts)[2], float* sm, int32_t& last_flag) {
     using C = Tile<D, F16Q, E4M3, HG>;
-    extern __shared__ __align__(16) float sm[];
+    constexpr bool solo = SOLO;
     float* sO = sm;                                   // [warp][row][LD]
     float* sM = sm + kPaWarps * C::ROWS * C::LD;      // [warp][row]
     float* sL = sM + kPaWarps * C::ROWS;
-    __shared__ uint64_t plan_sum[kPaWarps];
-    __shared__ Cut cuts[2];
-    __shared__ int32_t last_flag;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     const int H = a.n_kv * a.parts;                   // items a request
-
-    grid_dep_wait();
-
-    // ---- this CTA's share of all steps
     auto kept_at = [&](int r) { return kept_of(a, ld_index(a.lens + r)); };
     auto steps_of = [](const Kept& k) { return max((k.n + C::STEP - 1) / C::STEP, 1); };
-    PagedCuts plan;
-    {
-        const int per = (a.n_requests + kPaThreads - 1) / kPaThreads;
-        const int r0 = min(tid * per, a.n_requests), r1 = min(r0 + per, a.n_requests);
-        uint64_t mine = 0;
-        for (int r = r0; r < r1; r += 4) {
-            int32_t T[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) T[i] = r + i < r1 ? ld_index(a.lens + r + i) : 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (r + i < r1) mine += steps_of(kept_of(a, T[i])) + kPaItemCost;
-        }
-        uint64_t inc = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const uint64_t v = __shfl_up_sync(0xffffffffu, inc, o);
-            if (lane >= o) inc += v;
-        }
-        if (lane == 31) plan_sum[warp] = inc;
-        __syncthreads();
-        uint64_t all = 0, before = inc - mine;
-#pragma unroll
-        for (int w = 0; w < kPaWarps; ++w) {
-            if (w < warp) before += plan_sum[w];
-            all += plan_sum[w];
-        }
-        before *= H;
-        plan = paged_cuts(all * H, gridDim.x);
-        if (blockIdx.x >= plan.n) return;
-        const uint64_t b0 = paged_cut(plan, blockIdx.x), b1 = paged_cut(plan, blockIdx.x + 1);
-#pragma unroll 1
-        for (int i = 0; i < 2; ++i) {
-            const uint64_t b = i ? b1 : b0;
-            if (b >= plan.all) {
-                if (tid == 0) cuts[i] = Cut{plan.all, plan.all, a.n_requests, 0};
-            } else if (b >= before && b < before + mine * H) {
-                uint64_t at = before;
-                int r = r0, cost = 0;
-                for (; r < r1; ++r) {
-                    cost = steps_of(kept_at(r)) + kPaItemCost;
-                    if (b < at + (uint64_t)H * cost) break;
-                    at += (uint64_t)H * cost;
-                }
-                Cut c;
-                c.r = r;
-                c.item = (int)div_u64(b - at, cost);
-                c.item_at = at + (uint64_t)c.item * cost;
-                const int moves = paged_cut_moves(plan, (int)(b - c.item_at), cost);
-                c.at = moves < 0 ? c.item_at : b;
-                if (moves > 0) {                                 // on to the next item
-                    c.item_at += cost;
-                    c.at = c.item_at;
-                    if (++c.item == H) c.item = 0, ++c.r;
-                }
-                cuts[i] = c;
-            }
-        }
-        __syncthreads();
-    }
-    const int length = (int)((int64_t)cuts[1].at - (int64_t)cuts[0].at);
-    if (length <= 0) return;
+    auto tiles_of = [](const Kept& k) { return (k.n + C::KT - 1) / C::KT; };
+    const int n_items = a.n_requests * H, workers = kPaWarps * gridDim.x, worker = warp * gridDim.x + blockIdx.x;
+    const int length = solo ? 0 : (int)((int64_t)cuts[1].at - (int64_t)cuts[0].at);
+    if (solo ? worker >= n_items : length <= 0) return;
 
     auto enter = [&](Work& w) {
+        if (solo) {
+            w.lo = 0;
+            w.hi = w.steps = max(tiles_of(w.kept), 1);
+            return;
+        }
         w.steps = steps_of(w.kept);
         w.lo = max(-w.pos, 0);
         w.hi = min(w.steps, length - w.pos);
     };
     auto advance = [&](const Work& w, Work& x) {
         x = w;
+        if (solo) {
+            if (workers >= n_items - (w.r * H + w.item)) return false;
+            const int i = w.r * H + w.item + workers;
+            x.r = i / H;
+            x.item = i - x.r * H;
+            x.kept = kept_at(x.r);
+            enter(x);
+            return true;
+        }
         x.pos = w.pos + w.steps + kPaItemCost;
         if (x.pos >= length) return false;
         if (++x.item == H) {
@@ -377,9 +331,9 @@ __global__ void __launch_bounds__(kPaThreads, (Tile<D, F16Q, E4M3, HG>::CTAS)) p
         return true;
     };
     Work w;
-    w.r = cuts[0].r;
-    w.item = cuts[0].item;
-    w.pos = (int)((int64_t)cuts[0].item_at - (int64_t)cuts[0].at);
+    w.r = solo ? worker / H : cuts[0].r;
+    w.item = solo ? worker % H : cuts[0].item;
+    w.pos = solo ? 0 : (int)((int64_t)cuts[0].item_at - (int64_t)cuts[0].at);
     w.kept = kept_at(w.r);
     enter(w);
 
@@ -411,10 +365,11 @@ __global__ void __launch_bounds__(kPaThreads, (Tile<D, F16Q, E4M3, HG>::CTAS)) p
     auto valid_of = [&](uint32_t off) { return __ballot_sync(0xffffffffu, off != ~0u) & kFull; };
     // key `j` of the item's kept ones, if it is one of this CTA's
     auto ask = [&](const Work& w, int32_t j) {
-        return key_at(a, w.kept, a.pool.table + (int64_t)w.r * a.pool.max_pages, j < w.hi * C::STEP ? j : 0x7fffffff,
+        return key_at(a, w.kept, a.pool.table + (int64_t)w.r * a.pool.max_pages, solo || j < w.hi * C::STEP ? j : 0x7fffffff,
                       (uint32_t)(w.item / a.parts) * a.pool.head_u);
     };
-    auto first_key = [&](const Work& w) { return (w.lo * kPaWarps + warp) * C::KT + (lane & (C::KT - 1)); };
+    const int stride = solo ? C::KT : C::STEP;
+    auto first_key = [&](const Work& w) { return (solo ? 0 : (w.lo * kPaWarps + warp) * C::KT) + (lane & (C::KT - 1)); };
     // the item's first query head, and how many heads it has
     auto head0_of = [&](const Work& w) { const int kv = w.item / a.parts; return kv * a.group + (w.item - kv * a.parts) * kPagedRows; };
     auto rows_of = [&](const Work& w) { return min(kPagedRows, (w.item / a.parts + 1) * a.group - head0_of(w)); };
@@ -445,7 +400,7 @@ __global__ void __launch_bounds__(kPaThreads, (Tile<D, F16Q, E4M3, HG>::CTAS)) p
 
     int32_t j = first_key(w);
     uint32_t off = key_offset(a, ask(w, j));
-    KeyAt next = ask(w, j + C::STEP);
+    KeyAt next = ask(w, j + stride);
     uint32_t valid = valid_of(off);
     load_K(off);
     load_V(off);
@@ -503,8 +458,8 @@ __global__ void __launch_bounds__(kPaThreads, (Tile<D, F16Q, E4M3, HG>::CTAS)) p
 
         for (int s = w.lo; s < w.hi; ++s) {
             const uint32_t off_next = key_offset(a, next);
-            j += C::STEP;
-            next = ask(w, j + C::STEP);
+            j += stride;
+            next = ask(w, j + stride);
             const uint32_t valid_next = valid_of(off_next);
             const bool more = s + 1 < w.hi;
             if (valid == 0u) {                        // a short item: nothing for this warp
@@ -634,12 +589,47 @@ __global__ void __launch_bounds__(kPaThreads, (Tile<D, F16Q, E4M3, HG>::CTAS)) p
             load_V(off);
             load_Q(x);
             j = first_key(x);
-            next = ask(x, j + C::STEP);
+            next = ask(x, j + stride);
         };
         const bool whole = w.lo == 0 && w.hi == w.steps;
         if (another && whole) request();              // (not across the call that joins pieces)
 
         const int head0 = head0_of(w), rows = rows_of(w);
+        const float v_scale = E4M3 && a.v_scale != nullptr ? a.v_scale[kv] : 1.f;
+        if (solo) {
+            // the rows as they lie in registers: neighbouring components of heads 2t and 2t + 1
+#pragma unroll
+            for (int hg = 0; hg < HG; ++hg)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    float sum = l[hg][k];
+                    sum += __shfl_xor_sync(0xffffffffu, sum, 4);
+                    sum += __shfl_xor_sync(0xffffffffu, sum, 8);
+                    sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+                    const int row = hg * 8 + 2 * t + k;
+                    if (row < rows) {
+                        const float inv = sum == 0.f ? 0.f : v_scale / sum;
+                        char* to = a.O + (((int64_t)w.r * a.n_heads + head0 + row) * D + g * C::VE) * 2;
+#pragma unroll
+                        for (int c = 0; c < C::VC; ++c)
+#pragma unroll
+                            for (int e = 0; e < C::VE; e += 8) {
+                                uint32_t v[4];
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    const float (&acc)[4] = o[(c * C::VE + e) / 2 + i][hg];
+                                    v[i] = pack2<F16Q>(acc[k] * inv, acc[k + 2] * inv);
+                                }
+                                *reinterpret_cast<uint4*>(to + (c * 8 * C::VE + e) * 2) = make_uint4(v[0], v[1], v[2], v[3]);
+                            }
+                        if (a.LSE != nullptr && g == 0)
+                            a.LSE[(int64_t)(head0 + row) * a.n_requests + w.r] = m[hg][k] * c_col[hg][k] * 0.6931471805599453f + logf(sum);
+                    }
+                }
+            if (!another) break;
+            w = x;
+            continue;
+        }
         // ---- the four warps' results, joined through shared memory
 #pragma unroll
         for (int hg = 0; hg < HG; ++hg)
@@ -670,7 +660,6 @@ __global__ void __launch_bounds__(kPaThreads, (Tile<D, F16Q, E4M3, HG>::CTAS)) p
 
         constexpr int PER = 4;                             // neighbouring columns a thread
         constexpr size_t kPart = kPartWords<D>;
-        const float v_scale = E4M3 && a.v_scale != nullptr ? a.v_scale[kv] : 1.f;
         const Rows<D, F16Q> out{a.O + ((int64_t)w.r * a.n_heads + head0) * D * 2,
                                 a.LSE == nullptr ? nullptr : a.LSE + (int64_t)head0 * a.n_requests + w.r, a.n_requests, v_scale};
         float* my_part = a.part + (2 * blockIdx.x + (w.lo == 0)) * kPart;
@@ -732,6 +721,100 @@ __global__ void __launch_bounds__(kPaThreads, (Tile<D, F16Q, E4M3, HG>::CTAS)) p
         w = x;
         __syncthreads();                    // shared memory is free for the next item
     }
+}
+
+template <int D, bool F16Q, bool E4M3, int HG>
+__global__ void __launch_bounds__(kPaThreads, (Tile<D, F16Q, E4M3, HG>::CTAS)) paged_attn_kernel(const PagedAttnArgs a) {
+    using C = Tile<D, F16Q, E4M3, HG>;
+    extern __shared__ __align__(16) float sm[];
+    __shared__ uint64_t plan_sum[kPaWarps];
+    __shared__ uint32_t plan_longest[kPaWarps];
+    __shared__ Cut cuts[2];
+    __shared__ int32_t last_flag;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int H = a.n_kv * a.parts;                   // items a request
+
+    grid_dep_wait();
+
+    // ---- this CTA's share of all steps
+    auto kept_at = [&](int r) { return kept_of(a, ld_index(a.lens + r)); };
+    auto steps_of = [](const Kept& k) { return max((k.n + C::STEP - 1) / C::STEP, 1); };
+    auto tiles_of = [](const Kept& k) { return (k.n + C::KT - 1) / C::KT; };
+    PagedCuts plan;
+    bool solo;
+    {
+        const int per = (a.n_requests + kPaThreads - 1) / kPaThreads;
+        const int r0 = min(tid * per, a.n_requests), r1 = min(r0 + per, a.n_requests);
+        uint64_t mine = 0;
+        uint32_t longest = 0;
+        for (int r = r0; r < r1; r += 4) {
+            int32_t T[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) T[i] = r + i < r1 ? ld_index(a.lens + r + i) : 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (r + i < r1) {
+                    const Kept k = kept_of(a, T[i]);
+                    mine += steps_of(k) + kPaItemCost;
+                    longest = max(longest, (uint32_t)tiles_of(k));
+                }
+        }
+        uint64_t inc = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint64_t v = __shfl_up_sync(0xffffffffu, inc, o);
+            if (lane >= o) inc += v;
+        }
+        longest = __reduce_max_sync(0xffffffffu, longest);
+        if (lane == 31) {
+            plan_sum[warp] = inc;
+            plan_longest[warp] = longest;
+        }
+        __syncthreads();
+        uint64_t all = 0, before = inc - mine;
+#pragma unroll
+        for (int w = 0; w < kPaWarps; ++w) {
+            if (w < warp) before += plan_sum[w];
+            all += plan_sum[w];
+            longest = max(longest, plan_longest[w]);
+        }
+        before *= H;
+        // (every CTA comes to the same answer: same numbers, same order)
+        solo = longest <= 2 && a.n_requests * H > (int)gridDim.x;       // (the same for every CTA)
+        plan = paged_cuts(all * H, gridDim.x);
+        if (!solo && blockIdx.x >= plan.n) return;
+        const uint64_t b0 = paged_cut(plan, blockIdx.x), b1 = paged_cut(plan, blockIdx.x + 1);
+#pragma unroll 1
+        for (int i = 0; i < 2 && !solo; ++i) {
+            const uint64_t b = i ? b1 : b0;
+            if (b >= plan.all) {
+                if (tid == 0) cuts[i] = Cut{plan.all, plan.all, a.n_requests, 0};
+            } else if (b >= before && b < before + mine * H) {
+                uint64_t at = before;
+                int r = r0, cost = 0;
+                for (; r < r1; ++r) {
+                    cost = steps_of(kept_at(r)) + kPaItemCost;
+                    if (b < at + (uint64_t)H * cost) break;
+                    at += (uint64_t)H * cost;
+                }
+                Cut c;
+                c.r = r;
+                c.item = (int)div_u64(b - at, cost);
+                c.item_at = at + (uint64_t)c.item * cost;
+                const int moves = paged_cut_moves(plan, (int)(b - c.item_at), cost);
+                c.at = moves < 0 ? c.item_at : b;
+                if (moves > 0) {                                 // on to the next item
+                    c.item_at += cost;
+                    c.at = c.item_at;
+                    if (++c.item == H) c.item = 0, ++c.r;
+                }
+                cuts[i] = c;
+            }
+        }
+        __syncthreads();
+    }
+    if (solo) attend<D, F16Q, E4M3, HG, true>(a, plan, cuts, sm, last_flag);
+    else attend<D, F16Q, E4M3, HG, false>(a, plan, cuts, sm, last_flag);
 }
 
 template <int D, bool F16Q, bool E4M3, int HG>

@@ -409,14 +409,14 @@ typedef struct pafu_paged_cache {
     int64_t page_stride, token_stride, head_stride;    /* in elements of the pools */
     void* K;                       /* device, 16-byte aligned */
     void* V;
-    const float* k_scale;          /* device fp32 [n_kv_heads], positive; NULL = 1.  Only with PAFU_TYPE_E4M3 */
+    const float* k_scale;          /* device fp32 [n_kv_heads], positive normal numbers; NULL = 1.  Only with PAFU_TYPE_E4M3 */
     const float* v_scale;
     int32_t* table;                /* device int32 [n_requests, max_pages], contiguous; NULL if n_requests is 0 */
 } pafu_paged_cache;
 
 /* Workspace of the three calls below: PAFU_PAGED_HEADER_BYTES that the caller zeroes once after allocating (the status
  * header that pafu_workspace_status reads, and counters that are zero again at the end of every call), then scratch.
- * 256-byte aligned.  It serves caches of the same d_head and any other geometry (0 = invalid cache), one call at a time: calls that may
+ * 256-byte aligned.  The size depends on d_head alone (0 = invalid cache); one workspace serves one call at a time: calls that may
  * overlap on the GPU - two streams, two captured graphs that run side by side - need a workspace each.  It is not for the
  * calls above: what those leave behind the header would be taken for counters. */
 #define PAFU_PAGED_HEADER_BYTES 12800
@@ -451,7 +451,7 @@ pafu_status pafu_paged_tables(const pafu_paged_cache* cache, const int32_t* len_
  * slots[i] % page_size), rows with a negative slot go nowhere.  16-bit pools of the rows' type take copies, bit for bit; e4m3 pools take
  * x * (1 / scale) rounded to the nearest e4m3 value, ties to even, beyond 448 (infinities too) to 448, NaN to NaN.
  * A slot past the pool is left out and reported (PAFU_ERR_BAD_PAGE).  Where two rows name the same slot, what it holds
- * afterwards is not defined.
+ * afterwards is not defined.  cache->K and cache->V must differ.
  *   Kn, Vn    device [n_tokens, n_kv_heads, d_head] of cache->type with strides ld_token and ld_head in elements (multiples of 8),
  *             16-byte aligned, e.g. parts of fused query/key/value rows; they must not overlap the pools
  *   slots     device int64 [n_tokens]

@@ -376,8 +376,8 @@ class PagedCache:
     """One layer's paged key/value cache: pools K and V [n_pages, page_size, n_kv_heads, d_head] (any strides with contiguous
     rows, the same for both; bf16, fp16 or float8_e4m3fn), the block table [n_requests, max_pages] int32, and for 8-bit pools
     a scale a key head.  n_heads query heads share the key heads in groups; dtype is the type of
-    queries, new rows and outputs (default: the pools').  Only pointers are kept beside the tensors, so they are
-    updated in place."""
+    queries, new rows and outputs (default: the pools').  The tensors are kept, and updated
+    in place; a call's own tensors must lie on the same device, and that must be the current one."""
 
     def __init__(self, K: torch.Tensor, V: torch.Tensor, table: torch.Tensor, n_heads: int,
                  dtype: Optional[torch.dtype] = None, k_scale: Optional[torch.Tensor] = None,
@@ -401,16 +401,13 @@ class PagedCache:
                              None if k_scale is None else k_scale.data_ptr(),
                              None if v_scale is None else v_scale.data_ptr(), table.data_ptr())
         self._ref, self._q_shape = ctypes.byref(self.c), (self.n_requests, n_heads, d)
-        self._index = K.get_device()
+        self._index, self._lib = K.get_device(), lib()
 
 
-def _paged_stream(cache: PagedCache, where: str) -> int:
-    """The current stream; the cache's device must be the current one.  (These calls come once a layer and token: the short
-    way to the handle takes 0.2 us, torch.cuda.current_stream() 3 us.)"""
-    i = cache._index
-    if i < 0 or i != torch._C._cuda_getDevice():
-        raise PafuError(1, where)
-    return torch._C._cuda_getCurrentRawStream(i)
+# These calls come once a layer and token, so their way is short: the device and the stream are asked for directly (0.2 us;
+# torch.cuda.current_stream() takes 3 us), and what a call checks is one expression.
+_device_now = torch._C._cuda_getDevice
+_stream_of = torch._C._cuda_getCurrentRawStream
 
 
 def pafu_paged_workspace_bytes(cache: PagedCache) -> int:
@@ -421,9 +418,9 @@ def pafu_paged_tables(cache: PagedCache, len_old: torch.Tensor, len_new: torch.T
                       n_free: torch.Tensor, n_free_out: torch.Tensor, len_out: torch.Tensor, slots: torch.Tensor,
                       cu_new: torch.Tensor, ws: torch.Tensor) -> None:
     """Block tables and slot map of a step from the lengths before and after it, all on the device."""
-    R, i32, i, st = cache.n_requests, torch.int32, cache._index, _paged_stream(cache, "pafu_paged_tables")
-    if not (len_old.dtype is i32 and len_new.dtype is i32 and len_out.dtype is i32 and free_list.dtype is i32
-            and n_free.dtype is i32 and n_free_out.dtype is i32 and cu_new.dtype is i32 and slots.dtype is torch.int64
+    R, i32, i = cache.n_requests, torch.int32, cache._index
+    if not (i >= 0 and i == _device_now() and len_old.dtype is i32 and len_new.dtype is i32 and len_out.dtype is i32
+            and free_list.dtype is i32 and n_free.dtype is i32 and n_free_out.dtype is i32 and cu_new.dtype is i32 and slots.dtype is torch.int64
             and len_old.numel() == R and len_new.numel() == R and len_out.numel() == R and cu_new.numel() == R + 1
             and free_list.numel() == cache.n_pages and n_free.numel() == 1 and n_free_out.numel() == 1
             and len_old.is_contiguous() and len_new.is_contiguous() and len_out.is_contiguous() and cu_new.is_contiguous()
@@ -431,22 +428,22 @@ def pafu_paged_tables(cache: PagedCache, len_old: torch.Tensor, len_new: torch.T
             and len_old.get_device() == len_new.get_device() == len_out.get_device() == free_list.get_device() == n_free.get_device()
             == n_free_out.get_device() == cu_new.get_device() == slots.get_device() == ws.get_device() == i):
         raise PafuError(1, "pafu_paged_tables")
-    status = lib().pafu_paged_tables(cache._ref, len_old.data_ptr(), len_new.data_ptr(), free_list.data_ptr(), n_free.data_ptr(),
-                                     n_free_out.data_ptr(), len_out.data_ptr(), slots.data_ptr(), slots.numel(), cu_new.data_ptr(),
-                                     ws.data_ptr(), ws.nbytes, st)
+    status = cache._lib.pafu_paged_tables(cache._ref, len_old.data_ptr(), len_new.data_ptr(), free_list.data_ptr(), n_free.data_ptr(),
+                                          n_free_out.data_ptr(), len_out.data_ptr(), slots.data_ptr(), slots.numel(), cu_new.data_ptr(),
+                                          ws.data_ptr(), ws.nbytes, _stream_of(i))
     if status:
         raise PafuError(status, "pafu_paged_tables")
 
 
 def pafu_paged_append(cache: PagedCache, Kn: torch.Tensor, Vn: torch.Tensor, slots: torch.Tensor, ws: torch.Tensor) -> None:
     """New tokens' rows Kn, Vn [n, n_kv_heads, d_head] (equal strides, contiguous rows) into the slots they are given."""
-    n, i, st, strides, dtype = slots.numel(), cache._index, _paged_stream(cache, "pafu_paged_append"), Kn.stride(), cache.dtype
-    if not (Kn.shape == (n, cache.n_kv_heads, cache.d_head) and Vn.shape == Kn.shape and Vn.stride() == strides and strides[2] == 1
-            and Kn.dtype is dtype and Vn.dtype is dtype and slots.dtype is torch.int64 and slots.is_contiguous() and ws.is_contiguous()
+    n, i, strides, dtype = slots.numel(), cache._index, Kn.stride(), cache.dtype
+    if not (i >= 0 and i == _device_now() and Kn.shape == (n, cache.n_kv_heads, cache.d_head) and Vn.shape == Kn.shape
+            and Vn.stride() == strides and strides[2] == 1 and Kn.dtype is dtype and Vn.dtype is dtype and slots.dtype is torch.int64 and slots.is_contiguous() and ws.is_contiguous()
             and Kn.get_device() == Vn.get_device() == slots.get_device() == ws.get_device() == i):
         raise PafuError(1, "pafu_paged_append")
-    status = lib().pafu_paged_append(cache._ref, Kn.data_ptr(), Vn.data_ptr(), strides[0], strides[1], slots.data_ptr(), n,
-                                     ws.data_ptr(), ws.nbytes, st)
+    status = cache._lib.pafu_paged_append(cache._ref, Kn.data_ptr(), Vn.data_ptr(), strides[0], strides[1], slots.data_ptr(), n,
+                                          ws.data_ptr(), ws.nbytes, _stream_of(i))
     if status:
         raise PafuError(status, "pafu_paged_append")
 
@@ -454,15 +451,15 @@ def pafu_paged_append(cache: PagedCache, Kn: torch.Tensor, Vn: torch.Tensor, slo
 def pafu_paged_attn(cache: PagedCache, Q: torch.Tensor, lens: torch.Tensor, O: torch.Tensor, LSE: Optional[torch.Tensor] = None,
                     n_sink: int = 0, n_recent: int = -1, scale: float = 0.0, ws: Optional[torch.Tensor] = None) -> None:
     """Attention of one new token a request, Q [n_requests, n_heads, d_head], over its pages."""
-    shape, i, st, strides, dtype = cache._q_shape, cache._index, _paged_stream(cache, "pafu_paged_attn"), Q.stride(), cache.dtype
-    if not (Q.shape == shape and O.shape == shape and strides[2] == 1 and Q.dtype is dtype and O.dtype is dtype and O.is_contiguous()
-            and lens.dtype is torch.int32 and lens.numel() == shape[0] and lens.is_contiguous() and ws is not None and ws.is_contiguous()
+    shape, i, strides, dtype = cache._q_shape, cache._index, Q.stride(), cache.dtype
+    if not (i >= 0 and i == _device_now() and Q.shape == shape and O.shape == shape and strides[2] == 1
+            and Q.dtype is dtype and O.dtype is dtype and O.is_contiguous() and lens.dtype is torch.int32 and lens.numel() == shape[0] and lens.is_contiguous() and ws is not None and ws.is_contiguous()
             and Q.get_device() == O.get_device() == lens.get_device() == ws.get_device() == i
             and (LSE is None or LSE.dtype is torch.float32 and LSE.numel() == shape[0] * shape[1] and LSE.is_contiguous()
                  and LSE.get_device() == i)):
         raise PafuError(1, "pafu_paged_attn")
-    status = lib().pafu_paged_attn(cache._ref, Q.data_ptr(), strides[0], strides[1], lens.data_ptr(), n_sink, n_recent, scale,
-                                   O.data_ptr(), None if LSE is None else LSE.data_ptr(), ws.data_ptr(), ws.nbytes, st)
+    status = cache._lib.pafu_paged_attn(cache._ref, Q.data_ptr(), strides[0], strides[1], lens.data_ptr(), n_sink, n_recent, scale,
+                                        O.data_ptr(), None if LSE is None else LSE.data_ptr(), ws.data_ptr(), ws.nbytes, _stream_of(i))
     if status:
         raise PafuError(status, "pafu_paged_attn")
 

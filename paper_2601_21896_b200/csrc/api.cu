@@ -827,6 +827,7 @@ pafu_status pafu_paged_append(const pafu_paged_cache* c, const void* Kn, const v
     if (n_tokens == 0) return PAFU_OK;
     if (n_tokens > 0x7fffffffLL / c->n_kv_heads) return PAFU_ERR_UNSUPPORTED_SHAPE;
     if (Kn == nullptr || Vn == nullptr || slots == nullptr) return PAFU_ERR_INVALID_ARG;
+    if (c->K == c->V) return PAFU_ERR_INVALID_ARG;                   // a key and a value for every place
     size_t in_b = 0;
     e = rows_ok(n_tokens, ld_token, c->n_kv_heads, ld_head, c->d_head, &in_b);
     if (e != PAFU_OK) return e;
@@ -854,10 +855,11 @@ pafu_status pafu_paged_attn(const pafu_paged_cache* c, const void* Q, int64_t q_
     if (e != PAFU_OK) return e;
     if (!aligned16(Q) || !aligned16(O) || !aligned_to(lens, 4) || !aligned_to(LSE, 4)) return PAFU_ERR_MISALIGNED;
     const size_t out_b = (size_t)c->n_requests * c->n_heads * c->d_head * 2, lse_b = LSE != nullptr ? (size_t)c->n_requests * c->n_heads * 4 : 0;
-    if (ranges_overlap(O, out_b, Q, q_b) || ranges_overlap(O, out_b, LSE, lse_b) || ranges_overlap(LSE, lse_b, Q, q_b)) return PAFU_ERR_INVALID_ARG;
-    const size_t pool_b = paged_pool_bytes(c);
-    if (ranges_overlap(O, out_b, c->K, pool_b) || ranges_overlap(O, out_b, c->V, pool_b) || ranges_overlap(LSE, lse_b, c->K, pool_b) ||
-        ranges_overlap(LSE, lse_b, c->V, pool_b)) return PAFU_ERR_INVALID_ARG;
+    if (ranges_overlap(O, out_b, LSE, lse_b)) return PAFU_ERR_INVALID_ARG;
+    const size_t pool_b = paged_pool_bytes(c), len_b = (size_t)c->n_requests * 4;
+    struct { const void* p; size_t n; } in[] = {{Q, q_b}, {c->K, pool_b}, {c->V, pool_b}, {lens, len_b}, {c->table, len_b * (size_t)c->max_pages}};
+    for (const auto& x : in)
+        if (ranges_overlap(O, out_b, x.p, x.n) || ranges_overlap(LSE, lse_b, x.p, x.n)) return PAFU_ERR_INVALID_ARG;
     e = paged_ws_ok(c, ws, ws_bytes);
     if (e != PAFU_OK) return e;
     if (scale == 0.f) scale = 1.0f / sqrtf((float)c->d_head);

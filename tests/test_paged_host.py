@@ -121,6 +121,7 @@ def test_append_refuses_on_the_host(L):
     assert append(L, c, K=FAKE + pool - 512) == INVALID                      # rows inside the pools
     assert append(L, c, V=FAKE + GB) == INVALID
     assert append(L, c, V=FAKE + GB - 256) == INVALID
+    assert append(L, cache(V=FAKE)) == INVALID                               # one pool for keys and values
 
 
 def test_attention_refuses_on_the_host(L):
@@ -139,6 +140,8 @@ def test_attention_refuses_on_the_host(L):
     assert attn(L, c, O=FAKE + 12 * GB) == INVALID                            # over the queries
     assert attn(L, c, LSE=FAKE + 13 * GB + 64) == INVALID                     # inside the output
     assert attn(L, c, O=FAKE + 1024) == INVALID                               # inside the pools
+    assert attn(L, c, O=FAKE + 2 * GB) == INVALID                             # over the block table
+    assert attn(L, c, LSE=FAKE + 3 * GB + 12) == INVALID                      # over the lengths
 
 
 def test_binding_refuses_tensors_of_the_wrong_kind(L):

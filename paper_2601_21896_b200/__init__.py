@@ -1,5 +1,7 @@
 """PaFu-KV inference hot path for NVIDIA B200: score -> select -> compact -> chunk attention.
 
+Beside it a paged cache for many requests: block tables, rows into pages, attention of one new token.
+
 The product is the C-ABI CUDA library ``libpafu.so`` (see ``include/pafu.h``); this package is
 its thin Python binding plus the seeded workload generator.  Nothing here computes on the CPU.
 """

@@ -85,7 +85,7 @@ using namespace pafu;
 
 extern "C" {
 
-int32_t pafu_version(void) { return 1000; }
+int32_t pafu_version(void) { return 1001; }
 
 const char* pafu_status_string(pafu_status s) {
     switch (s) {

@@ -15,6 +15,11 @@
 // (2^-17 of a probability is lost then); fp16 keeps 2^-12, half a step of an fp16 output.
 // 8-bit caches are widened to fp16, which holds every e4m3 value; bf16 queries are scaled by a power of two a row so that
 // their largest component lies in [2^14, 2^15) and fp16 holds them to 2^-39 of it.
+// Measured: 64 requests of up to 8192 tokens, 32 heads over 8 key heads, 128, bf16 (1.15 GB): 179 us, 6.4 TB/s; 8 bits (0.57 GB, 40 over 8
+// heads): 96 us, 5.9 TB/s, where widening makes it 40 % of the issue slots.  The tensor cores are 14 to 18 % busy, so mma.sync's rate does
+// not bound it, and tcgen05 would need its rows in shared memory and P's transpose through tensor memory.  Staging the rows in
+// shared memory by cp.async instead (built: fragments from there, 8 and 16 KB a warp under way): 185 us with 12 warps an SM and 8 KB, 243 with 16 KB, since
+// what is left of L1 no longer holds tables and spills, 181 with 8 warps and 16 KB; 8 bits 105, 151, 99.
 //
 // Split over the length: every (request, group of heads) is an item of ceil(kept / step) steps (a step is one tile for each of
 // the four warps) and a fixed cost.  All items laid end to end are cut into equal shares, one a CTA, by arithmetic that every

@@ -784,7 +784,6 @@ __global__ void __launch_bounds__(kPaThreads, (Tile<D, F16Q, E4M3, HG>::CTAS)) p
             longest = max(longest, plan_longest[w]);
         }
         before *= H;
-        // (every CTA comes to the same answer: same numbers, same order)
         solo = longest <= 2 && a.n_requests * H > (int)gridDim.x;       // (the same for every CTA)
         plan = paged_cuts(all * H, gridDim.x);
         if (!solo && blockIdx.x >= plan.n) return;

@@ -406,8 +406,8 @@ class PagedCache:
 
 # These calls come once a layer and token, so their way is short: the device and the stream are asked for directly (0.2 us;
 # torch.cuda.current_stream() takes 3 us), and what a call checks is one expression.
-_device_now = torch._C._cuda_getDevice
-_stream_of = torch._C._cuda_getCurrentRawStream
+_device_now = getattr(torch._C, "_cuda_getDevice", lambda: -1)              # (absent from a torch without CUDA)
+_stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", lambda i: 0)
 
 
 def pafu_paged_workspace_bytes(cache: PagedCache) -> int:

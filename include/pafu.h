@@ -472,6 +472,8 @@ pafu_status pafu_paged_append(const pafu_paged_cache* cache, const void* Kn, con
  *   scale     softmax scale; 0 means 1 / sqrt(d_head)
  *   O         device [n_requests, n_heads, d_head] of cache->type, contiguous, out
  *   LSE       device fp32 [n_heads, n_requests] log-sum-exp of the scaled logits, or NULL
+ * Infinities and NaN among the kept keys and values make the outputs that they enter infinite or NaN (not always the same one that exact
+ * arithmetic would); what lies in places that are not kept never does.
  * A request without kept positions gets o = 0 and LSE = -inf.  Table entries that are no page of the pool are left out with their
  * tokens, lengths outside [0, max_pages * page_size] are cut to it, and both are reported (PAFU_ERR_BAD_PAGE).  The work is cut evenly
  * over the GPU whatever the lengths; results do not depend on timing.  n_requests * n_heads < 2^31. */

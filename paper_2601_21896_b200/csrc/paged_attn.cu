@@ -282,8 +282,12 @@ __device__ __noinline__ void join_pieces(float* parts, int first, int p0, int by
 #pragma unroll
             for (int k = 0; k < PER; ++k) x[k] += f * y[p][k];
         }
-        if (out != nullptr) out->store(row, d, x, top, sum);
-        else put_part<D>(piece(0), row, d, x, top, sum);
+        if (out != nullptr) {
+            out->store(row, d, x, top, sum);
+        } else {
+            __syncwarp();                                    // every lane has read piece p0's maximum and sum, which lane 0 overwrites
+            put_part<D>(piece(0), row, d, x, top, sum);
+        }
     }
 }
 

@@ -162,6 +162,19 @@ def test_attention_split_over_the_length(d, cache, lens):
     assert header_is_clean(x.ws)
 
 
+@pytest.mark.parametrize("d,type,cache,heads,lens", [(128, "bf16", "bf16", 16, [60000]), (64, "f16", "f16", 3, [40000, 2000]),
+                                                     (128, "f16", "e4m3", 8, [30000, 30000]), (64, "bf16", "e4m3", 12, [90000])])
+def test_pieces_joined_in_groups_repeat_themselves(d, type, cache, heads, lens):
+    """Items of more than 16 pieces, whose groups are joined in place of their first piece, up to three levels: what a warp overwrites
+    there its lanes have read, so every run gives the same bits."""
+    x = Paged(lens, heads, 1, d, 64, type=type, cache=cache, seed=heads)
+    O, LSE = x.attn()
+    x.check(O, LSE)
+    again = [x.attn() for _ in range(60)]
+    assert all(torch.equal(O, o) and torch.equal(LSE, s) for o, s in again)
+    assert header_is_clean(x.ws)
+
+
 @pytest.mark.parametrize("n", [600, 3000])
 def test_attention_of_many_requests(n):
     """More requests than threads share out, most of them short or empty."""

@@ -874,7 +874,7 @@ pafu_status launch_paged_attn(const pafu_paged_cache& c, const void* Q, int64_t 
     a.group = c.n_heads / c.n_kv_heads;
     a.parts = (a.group + kPagedRows - 1) / kPagedRows;
     a.sink = (int32_t)(n_sink < 0x7fffffff ? n_sink : 0x7fffffff);
-    a.recent = (int32_t)(n_recent < 0x7fffffff ? n_recent : 0x7fffffff);
+    a.recent = n_recent < 0 ? -1 : (int32_t)(n_recent < 0x7fffffff ? n_recent : 0x7fffffff);
     a.scale = scale * 1.4426950408889634f;
     a.k_scale = c.k_scale;
     a.v_scale = c.v_scale;

@@ -149,6 +149,14 @@ def test_attention_over_sink_and_recent(sink, recent):
     x.check(*x.attn(sink=sink, recent=recent), sink=sink, recent=recent)
 
 
+@pytest.mark.parametrize("recent", [-1, -2, -2 ** 31, -2 ** 31 - 1, -2 ** 32, -2 ** 33 + 5, -2 ** 63, 2 ** 63 - 1])
+@pytest.mark.parametrize("sink", [0, 2])
+def test_any_negative_recent_keeps_every_position(sink, recent):
+    """The whole range of n_recent: what its lower 32 bits are does not matter."""
+    x = Paged(EDGE, 4, 2, 64, 24)
+    x.check(*x.attn(sink=sink, recent=recent), sink=sink, recent=-1)
+
+
 @pytest.mark.parametrize("d,cache,lens", [(128, "bf16", [20000]), (128, "e4m3", [33333, 1, 5]), (64, "f16", [9999, 10000, 0, 64]), (128, "bf16", [4097] * 9),
                                           (128, "bf16", [150000])])
 def test_attention_split_over_the_length(d, cache, lens):

@@ -526,7 +526,9 @@ __device__ __forceinline__ void attend(const PagedAttnArgs& a, const PagedCuts& 
                     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
                     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
                     const float c = c_col[hg][k], base = top == -INFINITY ? 0.f : top * c;
-                    f[hg][k] = ex2(fmaf(m[hg][k], c, -base));
+                    // (the old maximum rounded as it was when the sums were taken relative to it: exactly 1 where it stays, since o is
+                    // left alone then.  As one fused operation it is 2 to the power of what rounding base lost, a tile after the other.)
+                    f[hg][k] = ex2(__fmul_rn(m[hg][k], c) - base);
                     moved |= top != m[hg][k];
                     m[hg][k] = top;
                     float sum = 0.f;

@@ -227,6 +227,39 @@ def test_attention_of_8_bit_caches_with_queries_beyond_fp16(power):
     x.check(*x.attn(scale=scale), scale=scale)
 
 
+@pytest.mark.parametrize("type,cache", [("bf16", "bf16"), ("f16", "f16"), ("bf16", "e4m3")])
+@pytest.mark.parametrize("lens,kv", [([7000], 1), ([2500] * 40, 16), ([3000, 30] * 30, 12)])
+@pytest.mark.parametrize("logit", [5.3, -37.1, 411.0, 20011.0, 100003.0])
+def test_sums_do_not_drift_along_a_long_item(logit, lens, kv, type, cache):
+    """Keys of one logit, one product each and so exact in fp32, times a factor that is not: sums over any number of tiles are taken relative to
+    the same rounded maximum.  The log-sum-exp is the logit plus log n.  Bounds: its two terms and their sum are rounded by 2^-24 each (the logarithm and the
+    factors by a few steps more: 2^-21), n equal terms are added in fp32 (n 2^-24); equal values come out as they are, but for
+    the sums' rounding, that of one probability (2^-11 for fp16, 2^-17 for bf16) and the output's."""
+    d, page = 128, 16
+    x = Paged([1] * len(lens), 2 * kv, kv, d, page, type=type, cache=cache)
+    count = [-(-n // page) for n in lens]
+    width, scale = max(count), 0.7331 * 2.0 ** -3
+    # one page serves all: every position holds the same key and the same value
+    K, V = (make_pool(1, page, kv, d, POOL[cache], "tokens", 0.0) for _ in range(2))
+    K[..., 5], V[..., :] = torch.tensor(64.0).to(POOL[cache]), torch.tensor(1.25).to(POOL[cache])
+    table = torch.zeros((len(lens), width), dtype=torch.int32, device="cuda")
+    ones = dict(k_scale=torch.ones(kv, device="cuda"), v_scale=torch.ones(kv, device="cuda")) if cache == "e4m3" else {}
+    c = pafu.PagedCache(K, V, table, 2 * kv, dtype=x.dtype, **ones)
+    Q = torch.zeros((len(lens), 2 * kv, d), device="cuda", dtype=x.dtype)
+    Q[..., 5] = logit / (64 * scale)
+    O, LSE = torch.full_like(Q, float("nan")), torch.empty((2 * kv, len(lens)), device="cuda")
+    pafu.pafu_paged_attn(c, Q, torch.tensor(lens, dtype=torch.int32, device="cuda"), O, LSE, scale=scale, ws=x.ws)
+    s = Q[..., 5].double() * 64 * float(torch.tensor(scale, dtype=torch.float32))
+    n = torch.tensor(lens, device="cuda").double()[:, None]
+    want = (s + torch.log(n)).T
+    off = (LSE.double() - want).abs() / (2.0 ** -21 * want.abs() + 2.0 ** -21 * s.abs().T + n.T * 2.0 ** -24 + 2.0 ** -21)
+    assert bool((off <= 1).all()), off.max().item()
+    eps = torch.finfo(x.dtype).eps / 2
+    rel = eps + (2.0 ** -17 if cache == "bf16" else 2.0 ** -11) + max(lens) * 2.0 ** -24 + 2.0 ** -20
+    err = (O.double() / 1.25 - 1).abs().max().item()
+    assert err <= rel, err
+
+
 def test_attention_reads_strided_queries_and_pools():
     """Queries inside fused rows; K and V inside one tensor, heads not contiguous."""
     x = Paged([130, 33], 6, 3, 128, 16)

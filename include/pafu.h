@@ -464,8 +464,9 @@ pafu_status pafu_paged_append(const pafu_paged_cache* cache, const void* Kn, con
  * own key and value are among them once pafu_paged_append has written them and lens counts them.
  * n_recent < 0 keeps every position; otherwise the n_sink first and the n_recent last ones (the attention-sink prefix and the recent
  * window of pafu_policy) are kept.  Positions outside are not read, whatever they hold.
- * fp32 accumulation and softmax; the probabilities enter the product as 16-bit values of the pools' type (fp16 for e4m3), for
- * bf16 followed by what that rounding leaves over.
+ * fp32 accumulation and softmax statistics; the probabilities enter the product as 16-bit values of the pools' type (fp16 for e4m3), for
+ * bf16 followed by what that rounding leaves over: each is off by at most 2^-17 of itself with bf16 pools, with the others by 2^-11 of itself
+ * or, below 2^-29 of the row's largest, by 2^-40 of that.
  *   Q         device [n_requests, n_heads, d_head] of cache->type with strides q_token and q_head in elements (multiples of 8), 16-byte
  *             aligned
  *   lens      device int32 [n_requests]

@@ -11,8 +11,11 @@
 // value row and a byte permute pairs the rows of two keys.  P goes from S^T's layout to the other product's by 8 x 8 transposes
 // in registers.  The rows' addresses come from the page table one tile ahead, so pages of any length, order and
 // stride cost the same and may end inside a tile.
-// Probabilities enter the product as 16-bit values.  For bf16 what that rounding leaves over follows in a second product
-// (2^-17 of a probability is lost then); fp16 keeps 2^-12, half a step of an fp16 output.
+// Probabilities p <= 1 enter the product as 16-bit values.  For bf16 what that rounding leaves over follows in a second product
+// (2^-17 of a probability is lost then).  fp16 (fp16 and 8-bit pages) rounds 2^15 p, so that its whole exponent range counts: at most 2^-11 of p is
+// lost, as rounding an fp16 output loses, or 2^-40 of the largest probability where p is below 2^-29 of it.  (p itself would be a subnormal below
+// 2^-14 and nothing below 2^-25: beside a first token that draws the attention that is every other one.)  A second product for fp16 pages,
+// measured: 0.3 to 0.7 % longer for up to 8 heads a key head, 5 % for 16, against errors that mostly cancel over the keys: left out.
 // 8-bit caches are widened to fp16, which holds every e4m3 value; bf16 queries are scaled by a power of two a row so that
 // their largest component lies in [2^14, 2^15) and fp16 holds them to 2^-39 of it.
 // Measured: 64 requests of up to 8192 tokens, 32 heads over 8 key heads, 128, bf16 (1.15 GB): 179 us, 6.4 TB/s; 8 bits (0.57 GB, 40 over 8
@@ -44,6 +47,7 @@ namespace {
 constexpr int kPaWarps = 4;
 constexpr int kPaThreads = kPaWarps * 32;
 constexpr int kPaJoin = 16;           // pieces that are joined at once
+constexpr float kPaLift = 15.f;       // power of two that lifts fp16 probabilities, and with them numerators and a lane's sums
 static_assert(3 * kPaTicketRow < kPagedTickets, "three counters a CTA, and the tables' own");
 
 struct PagedAttnArgs {
@@ -525,17 +529,18 @@ __device__ __forceinline__ void attend(const PagedAttnArgs& a, const PagedCuts& 
                     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
                     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
                     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-                    const float c = c_col[hg][k], base = top == -INFINITY ? 0.f : top * c;
-                    // (the old maximum rounded as it was when the sums were taken relative to it: exactly 1 where it stays, since o is
-                    // left alone then.  As one fused operation it is 2 to the power of what rounding base lost, a tile after the other.)
-                    f[hg][k] = ex2(__fmul_rn(m[hg][k], c) - base);
+                    const float c = c_col[hg][k], ref = top == -INFINITY ? 0.f : top, base = ref * c;
+                    // bf16: the old maximum rounded as it was when the sums were taken relative to it: exactly 1 where it stays, since o is
+                    // left alone then.  As one fused operation it is 2 to the power of what rounding base lost, a tile after the other.
+                    // fp16: relative to the maximum itself, for the rounding of a large one would leave fp16's range.
+                    f[hg][k] = C::F16 ? ex2((m[hg][k] - ref) * c) : ex2(__fmul_rn(m[hg][k], c) - base);
                     moved |= top != m[hg][k];
                     m[hg][k] = top;
                     float sum = 0.f;
 #pragma unroll
                     for (int i = 0; i < C::KT / 16; ++i) {
-                        S[i][hg][k] = ex2(fmaf(S[i][hg][k], c, -base));
-                        S[i][hg][k + 2] = ex2(fmaf(S[i][hg][k + 2], c, -base));
+                        S[i][hg][k] = ex2(C::F16 ? fmaf(S[i][hg][k] - ref, c, kPaLift) : fmaf(S[i][hg][k], c, -base));
+                        S[i][hg][k + 2] = ex2(C::F16 ? fmaf(S[i][hg][k + 2] - ref, c, kPaLift) : fmaf(S[i][hg][k + 2], c, -base));
                         sum += S[i][hg][k] + S[i][hg][k + 2];
                     }
                     l[hg][k] = l[hg][k] * f[hg][k] + sum;
@@ -606,7 +611,9 @@ __device__ __forceinline__ void attend(const PagedAttnArgs& a, const PagedCuts& 
         if (another && whole) request();              // (not across the call that joins pieces)
 
         const int head0 = head0_of(w), rows = rows_of(w);
-        const float v_scale = E4M3 && a.v_scale != nullptr ? a.v_scale[kv] : 1.f;
+        constexpr float unlift = C::F16 ? 0x1p-15f : 1.f;     // sums are put right as they leave the registers, numerators at the end
+        static_assert(kPaLift == 15.f, "unlift");
+        const float v_scale = (E4M3 && a.v_scale != nullptr ? a.v_scale[kv] : 1.f) * unlift;
         if (solo) {
             // the rows as they lie in registers: neighbouring components of heads 2t and 2t + 1
 #pragma unroll
@@ -617,6 +624,7 @@ __device__ __forceinline__ void attend(const PagedAttnArgs& a, const PagedCuts& 
                     sum += __shfl_xor_sync(0xffffffffu, sum, 4);
                     sum += __shfl_xor_sync(0xffffffffu, sum, 8);
                     sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+                    sum *= unlift;
                     const int row = hg * 8 + 2 * t + k;
                     if (row < rows) {
                         const float inv = sum == 0.f ? 0.f : v_scale / sum;
@@ -653,7 +661,7 @@ __device__ __forceinline__ void attend(const PagedAttnArgs& a, const PagedCuts& 
                 const int row = hg * 8 + 2 * t + k;
                 if (g == 0) {
                     sM[warp * C::ROWS + row] = m[hg][k] * c_col[hg][k];
-                    sL[warp * C::ROWS + row] = sum;
+                    sL[warp * C::ROWS + row] = sum * unlift;
                 }
                 if (row < rows) {
                     float* to = sO + (warp * C::ROWS + row) * C::LD + g * C::VE;

@@ -260,6 +260,100 @@ def test_sums_do_not_drift_along_a_long_item(logit, lens, kv, type, cache):
     assert err <= rel, err
 
 
+def sink_and_tail(n, margin, spread, d, type, cache, heads, kv, seed=0, sink_at=0, sink_value=0.0):
+    """One request of n tokens whose key `sink_at` has a logit of about `margin` above the others', and a value of zero; the others'
+    logits are all equal (spread 0) or vary, their values are positive, so that what is lost of their weights does not cancel."""
+    x = Paged([n], heads, kv, d, 16, type=type, cache=cache, seed=seed)
+    g = torch.Generator("cuda").manual_seed(seed + 1)
+    k = torch.randn((n, kv, d), device="cuda", generator=g) * spread
+    k[..., 0] = 0.0
+    k[sink_at] = 0.0
+    k[sink_at, :, 0] = margin * math.sqrt(d) / 128.0
+    v = torch.rand((n, kv, d), device="cuda", generator=g) + 0.5
+    v[sink_at] = sink_value
+    x.Q[..., 0] = 128.0
+    t = torch.arange(n, device="cuda")
+    at = x.table[0].long()[t // 16]
+    for pool, scale, keep, new in ((x.cache.K, x.ks, x.k, k), (x.cache.V, x.vs, x.v, v)):
+        new = (new if scale is None else (new / scale[:, None]).clamp(-448, 448)).to(POOL[cache])
+        raw = torch.uint8 if cache == "e4m3" else torch.int16
+        pool.view(raw)[at, t % 16] = new.view(raw)
+        keep[0] = new.double() if scale is None else new.double() * scale.double()[:, None]
+    return x
+
+
+@pytest.mark.parametrize("type,cache", [("bf16", "bf16"), ("f16", "f16"), ("bf16", "e4m3"), ("f16", "e4m3")])
+@pytest.mark.parametrize("n,spread,d,heads,kv", [(40, 0.0, 64, 4, 1), (300, 0.0, 128, 3, 3), (2000, 0.0, 128, 8, 1), (2000, 1.0, 64, 16, 1),
+                                                 (20000, 0.5, 128, 4, 2), (100000, 1.0, 128, 4, 1)])
+@pytest.mark.parametrize("margin", [8, 12, 16, 20])
+def test_small_probabilities_beside_a_sink(margin, n, spread, d, heads, kv, type, cache):
+    """A first token that draws the attention while its value is nothing: the output is the others', whose probabilities are e^-8 to e^-20 of
+    the largest.  Bound: as in Paged.check, with the probabilities' rounding as the format has it.  fp16 rounds p 2^15 (p <= 1) by at
+    most 2^-11 of it, or 2^-25 where that is a subnormal: 2^-40 of the largest probability.  bf16 leaves 2^-17 after its second term."""
+    x = sink_and_tail(n, margin, spread, d, type, cache, heads, kv, seed=n + margin)
+    O, LSE = x.attn()
+    G, scale, eps = heads // kv, 1.0 / math.sqrt(d), torch.finfo(x.dtype).eps / 2
+    one_term = cache != "bf16"
+    for h in range(kv):
+        q, k, v = x.Q[0, h * G:(h + 1) * G].double(), x.k[0][:, h], x.v[0][:, h]
+        s = q @ k.T * scale
+        w = torch.softmax(s, -1)
+        want, lse = w @ v, torch.logsumexp(s, -1)
+        assert bool((s[:, 0] - s[:, 1:].mean(-1) > 0.85 * margin).all())                    # the keys' own rounding included
+        size = (q.abs() @ k.abs().T * scale).amax(-1)
+        delta = (d + 8) * 2.0 ** -23 * size + 2.0 ** -22 * (s.abs().amax(-1) + 2)
+        rel = 2 * delta + (2.0 ** -11 if one_term else 2.0 ** -17) + n * 2.0 ** -24 + 2.0 ** -21
+        lost = 2.0 ** -40 * w.amax(-1, keepdim=True) * v.sum(0) if one_term else 0.0
+        tol = eps * want.abs() + rel[:, None] * want * (1 + eps) + lost + torch.finfo(x.dtype).smallest_normal * eps
+        got = O[0, h * G:(h + 1) * G].double()
+        worst = ((got - want).abs() / tol).max().item()
+        assert worst <= 1, (h, worst, ((got - want).abs() / want).max().item())
+        off = (LSE[h * G:(h + 1) * G, 0].double() - lse).abs()
+        assert bool((off <= delta + 2.0 ** -22 * lse.abs() + n * 2.0 ** -24 + 2.0 ** -21).all()), (h, off.max().item())
+
+
+def test_small_probabilities_of_many_short_items():
+    """The same for items that a warp takes by itself, and for a sink that comes last: what is already summed is scaled down."""
+    for sink_at in (0, 29):
+        x = sink_and_tail(30, 16, 0.0, 128, "f16", "f16", 2, 1, sink_at=sink_at)
+        one, one_lse = x.attn()
+        many = 400
+        table = x.table.repeat(many, 1)
+        cache = pafu.PagedCache(x.cache.K, x.cache.V, table, 2)
+        Q, lens = x.Q.repeat(many, 1, 1), x.len_t.repeat(many)
+        O, LSE = torch.empty_like(Q), torch.empty((2, many), device="cuda")
+        pafu.pafu_paged_attn(cache, Q, lens, O, LSE, ws=x.ws)
+        s = x.Q[0].double() @ x.k[0][:, 0].T / math.sqrt(128)
+        want, lse = torch.softmax(s, -1) @ x.v[0][:, 0], torch.logsumexp(s, -1)
+        for o, l in ((one, one_lse), (O, LSE)):
+            # one rounding each of probabilities and output, 2^-11; the logit of the sink, 136 products of up to 16 in all, and its exponential
+            # by 2^-18; twice the smallest step of an output
+            assert bool(((o.double() - want).abs() <= (2 * 2.0 ** -11 + 2 * 136 * 2.0 ** -23 * 16 + 2.0 ** -16) * want + 2.0 ** -24).all())
+            assert bool(((l.double() - lse[:, None]).abs() <= 136 * 2.0 ** -23 * 16 + 2.0 ** -17).all())
+
+
+@pytest.mark.parametrize("type,cache", [("bf16", "bf16"), ("f16", "f16"), ("bf16", "e4m3"), ("f16", "e4m3")])
+@pytest.mark.parametrize("n,sink_at", [(20, 3), (500, 0), (500, 499), (5000, 2500)])
+@pytest.mark.parametrize("size", [10, 20, 24, 28, 30])
+def test_huge_logits_leave_the_largest(size, n, sink_at, type, cache):
+    """A largest logit of about 2^size, which fp32 holds to whole numbers and less: the output is that key's value, and what rounding the
+    maximum leaves over cancels or does not arise.  The probability and the output are rounded by at most 2^-11 and eps / 2; the other keys' logits lie a
+    fifth of 2^size and more below and count for nothing."""
+    x = sink_and_tail(n, 20, 0.5, 128, type, cache, 4, 2, seed=n, sink_at=sink_at, sink_value=1.3125)
+    scale = 2.0 ** size / (20 * math.sqrt(128))
+    O, LSE = x.attn(scale=scale)
+    eps = torch.finfo(x.dtype).eps / 2
+    for h in range(2):
+        s = x.Q[0, 2 * h:2 * h + 2].double() @ x.k[0][:, h].T * float(torch.tensor(scale, dtype=torch.float32))
+        two = s.topk(2).values
+        assert bool((s.argmax(-1) == sink_at).all()) and bool((two[:, 0] - two[:, 1] > 0.2 * 2.0 ** size).all())
+        want = x.v[0][sink_at, h]
+        got = O[0, 2 * h:2 * h + 2].double()
+        assert bool(((got - want).abs() <= (eps + 2.0 ** -11 + 2.0 ** -20) * want.abs()).all()), (got - want).abs().max()
+        # the logit: its factor, its products' sum and their product are rounded, 136 steps of 2^-23 at most
+        assert bool(((LSE[2 * h:2 * h + 2, 0].double() - two[:, 0]).abs() <= 140 * 2.0 ** -23 * two[:, 0]).all())
+
+
 def test_attention_reads_strided_queries_and_pools():
     """Queries inside fused rows; K and V inside one tensor, heads not contiguous."""
     x = Paged([130, 33], 6, 3, 128, 16)

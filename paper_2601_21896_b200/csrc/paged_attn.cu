@@ -73,20 +73,21 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 
-// 16 (8) bytes of a row, or zeros.  Predicated in one piece: as a branch, or with a second copy of the loads for whole tiles, the loop
+// 16 (8) bytes of a row, or zeros.  Not through the read-only path: the append ahead may still write these rows while this kernel is
+// already resident (the times are the same).  Predicated in one piece: as a branch, or with a second copy of the loads for whole tiles, the loop
 // over the keys runs 4 to 8 % longer.  Rows of 64 bytes are fetched as such: two heads of a token share a 128-byte line, but
 // come at different times (16 heads of 64 in 8 bits, 1.08 GB: 354 us with whole lines, 313 so).
 #define PAFU_LD_ROW(HINT)                                                                                       \
     __device__ __forceinline__ void ld_row##HINT(uint32_t (&w)[4], const char* p, bool ok) {                    \
         w[0] = w[1] = w[2] = w[3] = 0u;                                                                         \
         asm volatile("{\n\t.reg .pred P;\n\tsetp.ne.b32 P, %5, 0;\n\t"                                          \
-                     "@P ld.global.nc.L1::no_allocate.L2::" #HINT "B.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"       \
+                     "@P ld.global.L1::no_allocate.L2::" #HINT "B.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"       \
                      : "+r"(w[0]), "+r"(w[1]), "+r"(w[2]), "+r"(w[3]) : "l"(p), "r"((int)ok) : "memory");       \
     }                                                                                                           \
     __device__ __forceinline__ void ld_row##HINT(uint32_t (&w)[2], const char* p, bool ok) {                    \
         w[0] = w[1] = 0u;                                                                                       \
         asm volatile("{\n\t.reg .pred P;\n\tsetp.ne.b32 P, %3, 0;\n\t"                                          \
-                     "@P ld.global.nc.L1::no_allocate.L2::" #HINT "B.v2.u32 {%0, %1}, [%2];\n\t}"               \
+                     "@P ld.global.L1::no_allocate.L2::" #HINT "B.v2.u32 {%0, %1}, [%2];\n\t}"               \
                      : "+r"(w[0]), "+r"(w[1]) : "l"(p), "r"((int)ok) : "memory");                               \
     }
 PAFU_LD_ROW(64)

@@ -458,6 +458,34 @@ print("fine")
     assert r.returncode == 0 and "fine" in r.stdout, r.stdout + r.stderr
 
 
+@pytest.mark.parametrize("captured", [False, True])
+def test_attention_sees_rows_written_just_ahead(captured):
+    """Rows of the same places written over and over, the attention launched right behind each time: it has read the new ones."""
+    lens = [64, 1, 40]
+    x = Paged(lens, 4, 2, 128, 16)
+    places = [[int(x.table[r, t // 16]) * 16 + t % 16 for t in range(n)] for r, n in enumerate(lens)]
+    slots = torch.tensor(sum(places, []), device="cuda")
+    rows = torch.randn((30, 2, len(slots), 2, 128), device="cuda").to(torch.bfloat16)
+    outs = [(torch.empty_like(x.Q), torch.empty((4, 3), device="cuda")) for _ in rows]
+
+    def steps():
+        for (k, v), (O, LSE) in zip(rows, outs):
+            pafu.pafu_paged_append(x.cache, k, v, slots, ws=x.ws)
+            pafu.pafu_paged_attn(x.cache, x.Q, x.len_t, O, LSE, ws=x.ws)
+
+    if captured:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            steps()
+        graph.replay()
+    else:
+        steps()
+    torch.cuda.synchronize()
+    for (k, v), (O, LSE) in zip(rows, outs):
+        x.k, x.v = list(k.double().split(lens)), list(v.double().split(lens))
+        x.check(O, LSE)
+
+
 def test_a_workspace_serves_one_cache_after_the_other():
     a, b = Paged([3000, 7], 8, 1, 128, 16, seed=1), Paged([2000] * 3, 4, 2, 64, 8, seed=2)
     for _ in range(3):

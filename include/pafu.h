@@ -441,6 +441,8 @@ size_t pafu_paged_workspace_bytes(const pafu_paged_cache* cache);
  * is negative or needs more than max_pages pages, or a *n_free outside [0, n_pages], no page changes hands: table,
  * free_list and the number of free pages stay, len_out = len_old, slots are all -1, cu_new all 0, and pafu_workspace_status reports
  * PAFU_ERR_NO_PAGES (the first two) or PAFU_ERR_BAD_PAGE (the others).
+ * A page that the step takes or gives back and that is no page of the pool (a damaged table or free list) is handed on as it stands: its
+ * new tokens get slot -1, the rest of the step is as usual, and PAFU_ERR_BAD_PAGE is reported.
  * Apart from the aliases named, outputs must not overlap anything else.  Of `cache` only page_size, max_pages, n_requests, n_pages
  * and table are looked at beyond the checks. */
 pafu_status pafu_paged_tables(const pafu_paged_cache* cache, const int32_t* len_old, const int32_t* len_new,

@@ -146,6 +146,12 @@ __global__ void __launch_bounds__(kTabThreads) paged_tables_kernel(const TablesA
         }
         return a.table + (int64_t)r * a.max_pages + x.want + i;
     };
+    // what is no page of the pool is handed on as it stands, and reported
+    auto is_page = [&](int32_t page) {
+        const bool yes = (uint32_t)page < a.n_pages;
+        if (!yes) *a.status = PAFU_ERR_BAD_PAGE;
+        return yes;
+    };
     // runs, entries of the free list, and the slot map's end side by side: no thread does one after the other
     const int64_t runs = ok ? all.runs : 0, pushed = ok ? max(height - all.need - F, (int64_t)0) : 0;
     const int64_t filled = ok ? all.tokens : 0, jobs = runs + pushed + (a.n_slots - filled + kTabRun - 1) / kTabRun;
@@ -167,12 +173,15 @@ __global__ void __launch_bounds__(kTabThreads) paged_tables_kernel(const TablesA
             int32_t* entry = a.table + (int64_t)r * a.max_pages + p;
             const int32_t page = ld_index(p < x.have ? entry : stack(height - 1 - ((int64_t)needed + p - x.have)));
             if (p >= x.have && first == p * (int32_t)a.page.d) *entry = page;
-            int64_t slot = (int64_t)page * a.page.d + (pos - p * (int32_t)a.page.d);
+            const bool place = is_page(page);                 // -1 otherwise: no slot, and not one that the append would take for padding unseen
+            const int64_t slot = (int64_t)page * a.page.d + (pos - p * (int32_t)a.page.d);
             int64_t* to = a.slots + token + (pos - x.old_len);
-            for (int k = 0; k < last - pos; ++k) to[k] = slot + k;
+            for (int k = 0; k < last - pos; ++k) to[k] = place ? slot + k : -1;
         } else if (job < runs + pushed) {
             const int64_t v = F + job - runs;
-            a.free_list[v] = ld_index(stack(v));
+            const int32_t page = ld_index(stack(v));
+            is_page(page);
+            a.free_list[v] = page;
         } else {
             const int64_t first = filled + (job - runs - pushed) * kTabRun;
             for (int64_t k = first; k < min(first + kTabRun, a.n_slots); ++k) a.slots[k] = -1;

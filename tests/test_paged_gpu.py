@@ -735,6 +735,35 @@ def test_tables_refuse_as_a_whole():
     assert x.n_free == 0
 
 
+@pytest.mark.parametrize("bad", [-1, -2 ** 31, 40, 2 ** 31 - 1])
+@pytest.mark.parametrize("where", ["partly filled", "popped", "given back", "given back and taken"])
+def test_tables_report_what_is_no_page(where, bad):
+    """A table entry or free-list entry that is no page of the pool is handed on as it stands, its new tokens get no slot, and it is
+    reported: a lost row never looks like padding."""
+    n_pages, page, R, width = 40, 8, 3, 6
+    x = Tables(R, width, page, n_pages)
+    assert x.step([13, 20, 9], 42)                                        # two, three and two pages
+    table, free, n_free = x.table.copy(), x.free.copy(), x.n_free
+    if where == "partly filled":
+        table[0, 1], new = bad, [15, 21, 9]
+    elif where == "popped":
+        free[n_free - 1], new = bad, [13, 26, 9]                          # request 1 goes on to a new page
+    elif where == "given back":
+        table[2, 0], new = bad, [14, 21, 0]
+    else:
+        table[2, 1], new = bad, [14, 26, 0]                               # request 2's last page is request 1's next one
+    x.t.copy_(torch.from_numpy(table))
+    x.f.copy_(torch.from_numpy(free))
+    want = plain_tables(page, [13, 20, 9], new, table, free, n_free, 12, n_pages)
+    slots, cu = torch.full((12,), 99, dtype=torch.int64, device="cuda"), torch.empty(R + 1, dtype=torch.int32, device="cuda")
+    pafu.pafu_paged_tables(x.cache, x.lens, torch.tensor(new, dtype=torch.int32, device="cuda"), x.f, x.nf, x.nf, x.lens, slots, cu, ws=x.ws)
+    assert pafu.pafu_workspace_status(x.ws) == BAD_PAGE
+    assert x.lens.tolist() == new and int(x.nf) == want[2] and cu.tolist() == want[4]
+    assert np.array_equal(x.t.cpu().numpy(), want[0]) and np.array_equal(x.f.cpu().numpy(), want[1])
+    assert slots.tolist() == [s if 0 <= s < n_pages * page else -1 for s in want[3]]
+    assert not bool(x.ws[256:12800].any())
+
+
 def test_tables_of_a_long_step():
     """More new tokens than a CTA takes; pages of one request given to another in the same step."""
     x = Tables(6, 3000, 16, 3200, seed=3)

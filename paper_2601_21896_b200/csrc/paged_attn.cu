@@ -530,7 +530,7 @@ __device__ __forceinline__ void attend(const PagedAttnArgs& a, const PagedCuts& 
                     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
                     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
                     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-                    const float c = c_col[hg][k], ref = top == -INFINITY ? 0.f : top, base = ref * c;
+                    const float c = c_col[hg][k], ref = top == -INFINITY ? 0.f : top, base = __fmul_rn(ref, c);
                     // bf16: the old maximum rounded as it was when the sums were taken relative to it: exactly 1 where it stays, since o is
                     // left alone then.  As one fused operation it is 2 to the power of what rounding base lost, a tile after the other.
                     // fp16: relative to the maximum itself, for the rounding of a large one would leave fp16's range.
@@ -661,7 +661,7 @@ __device__ __forceinline__ void attend(const PagedAttnArgs& a, const PagedCuts& 
                 sum += __shfl_xor_sync(0xffffffffu, sum, 16);
                 const int row = hg * 8 + 2 * t + k;
                 if (g == 0) {
-                    sM[warp * C::ROWS + row] = m[hg][k] * c_col[hg][k];
+                    sM[warp * C::ROWS + row] = __fmul_rn(m[hg][k], c_col[hg][k]);
                     sL[warp * C::ROWS + row] = sum * unlift;
                 }
                 if (row < rows) {

@@ -451,7 +451,8 @@ pafu_status pafu_paged_tables(const pafu_paged_cache* cache, const int32_t* len_
 
 /* New tokens' key and value rows into the pools: row i goes to slot slots[i] (page slots[i] / page_size, place
  * slots[i] % page_size), rows with a negative slot go nowhere.  16-bit pools of the rows' type take copies, bit for bit; e4m3 pools take
- * the e4m3 value nearest to x / scale, ties to even, beyond 448 (infinities too) 448, for NaN NaN.
+ * the e4m3 value nearest to x / scale, ties to even, beyond 448 (infinities too) 448, for NaN NaN (scales in [2^-100, 2^100]; beyond them a quotient
+ * that all but lies between two values may go to either).
  * A slot past the pool is left out and reported (PAFU_ERR_BAD_PAGE).  Where two rows name the same slot, what it holds
  * afterwards is not defined.  cache->K and cache->V must differ.
  *   Kn, Vn    device [n_tokens, n_kv_heads, d_head] of cache->type with strides ld_token and ld_head in elements (multiples of 8),

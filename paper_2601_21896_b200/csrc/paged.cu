@@ -20,7 +20,7 @@ namespace {
 // entries behind those that are read, the free list only entries above its top), apart from the lengths and the free count,
 // which may be updated in place; the CTA that counts itself out last writes those.  A step moves a few KB to MB: the
 // trips to memory and the searches that follow one another bound it.  2000 requests with 360000 new tokens: 11.9 us, 19 with a search
-// and a lookup for every token; 256 requests with one token each: 4.4 us, of which 1.9 are the lengths and the scan.
+// and a lookup for every token; 256 requests with one token each: 4.5 us, of which 1.9 are the lengths and the scan.
 constexpr int kTabThreads = 512;
 constexpr int kTabRun = 16;           // tokens of a run, at most
 
@@ -215,7 +215,7 @@ __global__ void __launch_bounds__(kTabThreads) paged_tables_kernel(const TablesA
 
 // ---------------------------------------------------------------------------------- append
 // Copies rows to their slots, 16 bytes of the cache a lane; 8-bit caches take 16 values (32 bytes of the row), divided by their
-// head's scale, rounded to nearest even and saturated.  Bound by the bytes (28080 rows of 12 x 128, bf16 to e4m3: 37 us, 6.1 TB/s; 4680 of
+// head's scale, rounded to nearest even and saturated.  Bound by the bytes (28080 rows of 12 x 128, bf16 to e4m3: 37 to 39 us, 6.1 to 5.8 TB/s; 4680 of
 // 40 x 128 copied: 27 us, 6.2 TB/s); for a few tokens by latency.
 struct AppendArgs {
     char* K;
@@ -253,8 +253,9 @@ __device__ __forceinline__ float2 widen16(uint32_t v) {
     return __bfloat1622float2(*reinterpret_cast<__nv_bfloat162*>(&v));
 }
 
-// Sixteen values.  (The test is made once for them: one value in 60000 is beside a border.  28080 rows: 35.0 us without it, 37.0 with it,
-// 39.3 with a test for each.)
+// Sixteen values.  (The test is made once for them: with a scale of full mantissa one value in 60000 is beside a border.  28080 rows: 35.0 us without
+// it, 37.0 with it, 39.3 with a test for each.  Without a scale, or with a power of two, one bf16 value in 8 and one fp16 value in 64 lies
+// on that grid, and zeros always do: every warp then takes the second loop, for quotients that were exact.  66 us for bf16 rows, 52 for fp16.)
 template <bool F16>
 __device__ __forceinline__ uint4 narrow16(const uint4& x, const uint4& y, float scale) {
     const uint32_t in[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
@@ -347,7 +348,10 @@ pafu_status launch_paged_tables(const pafu_paged_cache& c, const int32_t* len_ol
     a.cu_new = cu_new;
     a.status = static_cast<int32_t*>(ws) + kStatusWordPaged;
     a.ticket = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + kWsHeaderBytes) + kPagedTickets - 1;
-    // About one run a thread in a step that one CTA manages, then about 192 a CTA: their searches are bound by what an SM can issue.
+    // A CTA for every 192 jobs that the slots and requests may make, where one does not do; jobs are runs, mostly.  Jobs go to the CTAs 512 at a
+    // time, so the first ones take 512 each and the others none where there are fewer: with 360000 new tokens 48 of 148 work.  Pages given back are not
+    // in the count: 64 requests of 200000 tokens that end, 800000 pages, take 1340 us beside a slot map of 16 places, one CTA, and 19 us beside one
+    // of 200000.
     const int64_t jobs = n_slots / (kTabRun / 2) + c.n_requests, want = jobs <= kTabThreads ? 1 : (jobs + 191) / 192;
     const int64_t most = device_sm_count(), grid = want < most ? want : most;
     return cuda_ok(launch_dependent(paged_tables_kernel, dim3((unsigned)grid), dim3(kTabThreads), 0, stream, 1, a));

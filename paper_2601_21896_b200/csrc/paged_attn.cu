@@ -19,7 +19,7 @@
 // 8-bit caches are widened to fp16, which holds every e4m3 value; bf16 queries are scaled by a power of two a row so that
 // their largest component lies in [2^14, 2^15) and fp16 holds them to 2^-39 of it.
 // Measured: 64 requests of up to 8192 tokens, 32 heads over 8 key heads, 128, bf16 (1.15 GB): 179 us, 6.4 TB/s; 8 bits (0.57 GB, 40 over 8
-// heads): 96 us, 5.9 TB/s, where widening makes it 40 % of the issue slots.  The tensor cores are 14 to 18 % busy, so mma.sync's rate does
+// heads): 96 us, 5.9 TB/s, where widening takes 42 % of the ALU pipe (37 % of the issue slots are used).  The tensor cores are 14 to 18 % busy, so mma.sync's rate does
 // not bound it, and tcgen05 would need its rows in shared memory and P's transpose through tensor memory.  Staging the rows in
 // shared memory by cp.async instead (built: fragments from there, 8 and 16 KB a warp under way): 185 us with 12 warps an SM and 8 KB, 243 with 16 KB, since
 // what is left of L1 no longer holds tables and spills, 181 with 8 warps and 16 KB; 8 bits 105, 151, 99.
@@ -33,7 +33,8 @@
 // in groups of 16 first, by as many CTAs.
 // Where no item has more than two tiles and there are more items than CTAs, a warp takes whole items by itself ("solo"): nothing is
 // joined, no warp is idle on an item of few keys.  12000 items of up to 10 keys of 128: 66.8 us with four warps an item, 24.2 so.  From four
-// tiles on (2400 items of up to 64 keys) both take 24 us, and with fewer items than CTAs four warps are quicker.
+// tiles on (2400 items of up to 64 keys) both take 24 us, and with fewer items than CTAs four warps are quicker.  (One longer request is enough to have
+// four warps an item again: 300 requests of up to 10 tokens, 40 heads, and one of 1000: 83 us.)
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math.h>
@@ -76,7 +77,7 @@ __device__ __forceinline__ float ex2(float x) {
 // 16 (8) bytes of a row, or zeros.  Not through the read-only path: the append ahead may still write these rows while this kernel is
 // already resident (the times are the same).  Predicated in one piece: as a branch, or with a second copy of the loads for whole tiles, the loop
 // over the keys runs 4 to 8 % longer.  Rows of 64 bytes are fetched as such: two heads of a token share a 128-byte line, but
-// come at different times (16 heads of 64 in 8 bits, 1.08 GB: 354 us with whole lines, 313 so).
+// come at different times (16 heads of 64 in 8 bits, 1.08 GB: 365 us with whole lines, 343 so).
 #define PAFU_LD_ROW(HINT)                                                                                       \
     __device__ __forceinline__ void ld_row##HINT(uint32_t (&w)[4], const char* p, bool ok) {                    \
         w[0] = w[1] = w[2] = w[3] = 0u;                                                                         \
